@@ -32,7 +32,7 @@
  *     scored and attended over the tokens it holds; pool slots past seq_lens[b]
  *     may hold anything (NaN included) and never influence a result.
  *
- * Supported shapes: head_dim in {64, 128}; page_size in {4, 8, 16, 32, 64};
+ * Supported shapes: head_dim in {64, 128}; page_size in {4, 8, 16, 32, 64} (from 8 on with the 4-bit cache);
  * 1 <= G = Hq / Hkv <= 16; max_pages_per_seq <= TS_MAX_PAGES_PER_SEQ.
  */
 #ifndef TINYSERVE_H_
@@ -48,7 +48,9 @@ extern "C" {
 #define TS_MAX_PAGES_PER_SEQ 16384
 
 enum { TS_OUT_F32 = 0, TS_OUT_BF16 = 1 };
-enum { TS_KV_BF16 = 0, TS_KV_INT8 = 1, TS_KV_FP16 = 2 };
+enum { TS_KV_BF16 = 0, TS_KV_INT8 = 1, TS_KV_FP16 = 2, TS_KV_FP4 = 3 };
+#define TS_MAX_HEAD_DIM 128
+#define TS_MAX_AXES 4
 
 typedef enum ts_status {
   TS_OK = 0,
@@ -126,7 +128,30 @@ typedef struct ts_layout {
    * same quantisation inside its launch.  The attention over an INT8 cache
    * multiplies in IEEE half: the bf16 queries are converted (exactly, for
    * magnitudes from 2^-14 to 65504; smaller ones lose low bits, larger ones are
-   * taken as 65504), the int8 codes are exact. */
+   * taken as 65504), the int8 codes are exact.
+   * TS_KV_FP4: four bits a number, e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6 for the codes 0
+   * to 7, the sign in bit 3), one positive bf16 scale per token, KV head, and key or
+   * value; the number is code * scale.  k_pool points to one block of
+   * page_size * (d + 4) bytes per (physical page, head), kv_tile_stride bytes apart
+   * (0: dense; a multiple of 16); v_pool, k_scale and v_scale are not looked at.
+   * A block holds, in this order,
+   *   keys    [S][d/2]              two channels a byte, the even one in the low half
+   *   values  [S/8][d/64][16][4][4] four bytes are the eight tokens 8o .. 8o+7 of one
+   *                                 channel, the even token in a byte's low half;
+   *                                 channel c is word [c/64][c%16][(c/16)%4]
+   *   scales  bf16 [S] of the keys, then bf16 [S] of the values.
+   * page_size is at least 8.  Queries, appended tokens and metadata are bf16.
+   * Quantising a bf16 row: scale = max_c |x_c| / 6 in fp32, rounded up to bf16 (1 for
+   * a zero row), code = x_c / scale in fp32, to the nearest number, ties to the even
+   * code, no negative zero.  Rows should be finite: a NaN becomes 0, an infinity the
+   * largest number of its row's scale.  Boxes hold the numbers so stored, rounded
+   * outwards to bf16.  The attention multiplies in bf16 (numbers and queries are exact
+   * there).  The fused calls take several launches with this format, one after the
+   * other on the stream: scores, selection, attention, and the append ahead of them;
+   * no workgroup waits for another, cluster_size and wait_limit play no part, and
+   * ts_query_aware_decode_static refuses it (TS_ERR_UNSUPPORTED).  A workspace that
+   * has served another format serves this one, and the other way round, only after
+   * ts_workspace_init. */
   int32_t kv_format;
   /* How the fused calls (ts_query_aware_decode, ts_append_and_decode) spread one
    * (sequence, KV head) over workgroups.  0 (the default): automatic, about one
@@ -163,6 +188,90 @@ int ts_build_page_meta(const ts_layout* layout, void* stream);
  * sequence whose page j would be >= P_max is left unchanged. */
 int ts_append_token_meta(const ts_layout* layout, const void* k_new, const void* v_new,
                          int advance_seq_lens, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * From the projections to the cache: per-head norms, position rotation, and the
+ * append of any number of tokens.
+ * ------------------------------------------------------------------------- */
+
+/* What happens to a row of queries or keys (one head of one token, d numbers):
+ *   norm       y_c = x_c * w_c / sqrt(mean_c x_c^2 + norm_eps), where w is given
+ *   rotation   the pairs of channels (i, i + rot_dim/2), or (2i, 2i + 1) with
+ *              interleaved != 0, i < rot_dim/2, turn by their angle:
+ *              a' = a cos - b sin, b' = b cos + a sin; channels from rot_dim on
+ *              pass through.  rot_dim: a multiple of 8, at most d; 0 = no rotation.
+ * The sum of squares is taken in fp64, everything else in fp32 (each operation
+ * rounded by itself), and the row is rounded to 16 bits once, at the end; a row
+ * that is neither normed nor rotated keeps its bits.
+ *   cos_sin    fp32 [num_positions][rot_dim], 16-byte aligned: the rot_dim/2 cosines
+ *              of a position, then its rot_dim/2 sines
+ *   positions  int32 [num_axes][num_tokens]: each token's position on each axis; NULL
+ *              in ts_append_rows = the token's place in its sequence (one axis)
+ *   num_axes   1, or up to TS_MAX_AXES (time, height, width, ...); pair i turns by
+ *              the position on axis axis_of_pair[i] (not looked at with one axis)
+ * Positions are trusted to lie in [0, num_positions); one outside takes the nearest
+ * row of the table. */
+typedef struct ts_rotary {
+  int32_t rot_dim;
+  int32_t interleaved;
+  int32_t num_axes;
+  int32_t num_positions;
+  const float* cos_sin;
+  const int32_t* positions;
+  const float* q_norm;   /* fp32 [d], 16-byte aligned; NULL = no norm */
+  const float* k_norm;
+  float norm_eps;        /* not negative */
+  uint8_t axis_of_pair[TS_MAX_HEAD_DIM / 2];
+} ts_rotary;
+
+/* Rows as a projection leaves them: 16-bit numbers, token t's heads from
+ * base + t * stride on (strides in elements, multiples of 4; a token's heads d apart;
+ * pointers 8-byte aligned), so that q, k and v may be slices of one matrix.  The
+ * outputs may be the inputs themselves (same pointer and stride); otherwise they must
+ * not overlap them. */
+typedef struct ts_rows {
+  int32_t num_tokens;
+  int32_t format;        /* TS_KV_BF16 or TS_KV_FP16 (ts_rotate_rows; an append goes by its layout) */
+  const void* q;         /* [num_tokens][Hq][d] or NULL */
+  const void* k;         /* [num_tokens][Hkv][d] */
+  const void* v;
+  void* q_out;
+  void* k_out;           /* ts_rotate_rows only */
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t v_stride;
+  int64_t q_out_stride;
+  int64_t k_out_stride;
+} ts_rows;
+
+/* Norm and rotation of the queries (q -> q_out) and keys (k -> k_out) of num_tokens
+ * tokens; q or k may be NULL.  positions are required where rot_dim > 0.  head_dim 64
+ * or 128; num_tokens = 0 does nothing. */
+int ts_rotate_rows(const ts_rotary* rotary, const ts_rows* rows, int32_t num_q_heads, int32_t num_kv_heads,
+                   int32_t head_dim, void* stream);
+
+enum { TS_LENS_KEEP = 0, TS_LENS_ADVANCE = 1, TS_LENS_AFTER = 2 };
+
+/* Appends the tokens of rows to the cache (any kv_format), keys normed and rotated on
+ * the way (rotary NULL: neither), and, where q is given, writes the tokens' normed and
+ * rotated queries to q_out in the same launch.
+ *   cu_tokens  int32 [num_seqs + 1], device: sequence b has the tokens cu_tokens[b] ..
+ *              cu_tokens[b + 1] - 1 of rows, none, one or many; rows behind
+ *              cu_tokens[num_seqs] are neither read nor written.  NULL: one token for
+ *              each sequence (num_tokens = num_seqs).
+ *   lens       TS_LENS_KEEP: seq_lens are the lengths before the append and stay;
+ *              TS_LENS_ADVANCE: ... and are advanced (by a launch of its own behind the
+ *              append); TS_LENS_AFTER: they count the new tokens already and stay.
+ * Token i of a sequence of n_b new ones is stored at position (length before) + i; the
+ * boxes of the pages that receive tokens are opened or widened by the keys as stored, and
+ * come out as ts_append_token_meta's, token by token, would (but for the sign of a zero).  A sequence whose tokens do
+ * not all fit in max_pages_per_seq pages is left unchanged (its queries are written all
+ * the same); tokens of a page whose block-table entry is out of range are not stored
+ * and leave its box alone.  Slots behind the new tokens keep what they held.  16-bit
+ * rows are of the cache's type, bf16 with the INT8 and 4-bit caches.  A sequence must
+ * not share a page that receives tokens with another. */
+int ts_append_rows(const ts_layout* layout, const ts_rotary* rotary, const ts_rows* rows, const int32_t* cu_tokens,
+                   int32_t lens, void* stream);
 
 /* Eq. 2, step 1 of Algorithm 1.  q: bf16 [B][Hq][d].  scores: fp32
  * [B][Hkv][P_max]; entry (b, h, j) is the group-summed bound for j < P_b and
@@ -263,7 +372,8 @@ int ts_append_and_decode(const ts_layout* layout, const void* k_new, const void*
 
 /* Host-only (needs the device to be present): 1 if ts_append_and_decode runs
  * this layout as a single launch, 2 if it enqueues the append as a kernel of
- * its own first; a negative ts_status on error. */
+ * its own first, 5 with the 4-bit cache (append, lengths, scores, selection,
+ * attention); a negative ts_status on error. */
 int ts_append_and_decode_launches(const ts_layout* layout, int32_t max_topk);
 
 /* Host-only: bytes of workspace the three calls above need for this layout and

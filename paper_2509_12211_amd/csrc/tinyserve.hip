@@ -1,7 +1,10 @@
 // C-ABI entry points (include/tinyserve.h) and the kernels behind them.
 // gfx950 only.  Device code is in ts_*.h; this file holds the __global__
 // wrappers, the work decomposition, and the host-side validation / launches.
+#include "ts_fp4.h"
 #include "ts_fused.h"
+
+#include <string.h>
 
 #include <atomic>
 #include <mutex>
@@ -266,6 +269,8 @@ __global__ void fill_zero_kernel(int32_t* p, size_t n) {
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+static int fp4_block_bytes(const ts_layout* L) { return L->page_size * (L->head_dim + 4); }
+
 static int check_layout(const ts_layout* L) {
   if (!L) return TS_ERR_NULL;
   if (L->num_seqs <= 0 || L->num_q_heads <= 0 || L->num_kv_heads <= 0 || L->head_dim <= 0 ||
@@ -285,8 +290,15 @@ static int check_layout(const ts_layout* L) {
   if (L->keep_first_pages < 0 || L->keep_last_pages < 0) return TS_ERR_SHAPE;
   if (L->cluster_size < 0 || L->wait_limit < 0) return TS_ERR_SHAPE;
   if (L->out_format != TS_OUT_F32 && L->out_format != TS_OUT_BF16) return TS_ERR_UNSUPPORTED;
-  if (L->kv_format != TS_KV_BF16 && L->kv_format != TS_KV_INT8 && L->kv_format != TS_KV_FP16)
+  if (L->kv_format != TS_KV_BF16 && L->kv_format != TS_KV_INT8 && L->kv_format != TS_KV_FP16 &&
+      L->kv_format != TS_KV_FP4)
     return TS_ERR_UNSUPPORTED;
+  if (L->kv_format == TS_KV_FP4) {
+    if (L->page_size < 8) return TS_ERR_UNSUPPORTED;
+    if (L->kv_tile_stride != 0 &&
+        (L->kv_tile_stride < fp4_block_bytes(L) || L->kv_tile_stride % 16 != 0))
+      return TS_ERR_SHAPE;
+  }
   if (L->kv_format == TS_KV_INT8 && L->kv_tile_stride % 16 != 0) return TS_ERR_SHAPE;
   return TS_OK;
 }
@@ -295,12 +307,14 @@ static int check_layout(const ts_layout* L) {
 // K and V tiles, the block table, the lengths and, for the INT8 cache, the two
 // per-token scale arrays the kernels dereference.
 static int check_pool(const ts_layout* L) {
-  if (!L->k_pool || !L->v_pool || !L->block_table || !L->seq_lens) return TS_ERR_NULL;
+  if (!L->k_pool || !L->block_table || !L->seq_lens) return TS_ERR_NULL;
+  if (L->kv_format != TS_KV_FP4 && !L->v_pool) return TS_ERR_NULL;   // (4 bits: one block holds both)
   if (L->kv_format == TS_KV_INT8 && (!L->k_scale || !L->v_scale)) return TS_ERR_NULL;
   return TS_OK;
 }
 
 static int tile_stride_of(const ts_layout* L) {
+  if (L->kv_format == TS_KV_FP4) return L->kv_tile_stride ? L->kv_tile_stride : fp4_block_bytes(L);
   return L->kv_tile_stride ? L->kv_tile_stride : L->head_dim * L->page_size;
 }
 
@@ -358,9 +372,229 @@ static AttendParams attend_params(const ts_layout* L, const Plan& pl, const void
   return a;
 }
 
+// ---------------------------------------------------------------------------
+// The 4-bit cache
+// ---------------------------------------------------------------------------
+struct Fp4Plan {
+  int workgroups;
+  size_t off_done, off_part, attend_total, off_scores, off_sel, off_count, total;
+};
+
+// pages: the most pages a unit attends.  query_aware: room for the scores and lists between the launches of
+// a fused call, too.  Goes by the shape of the batch alone.
+static Fp4Plan make_fp4_plan(const ts_layout* L, int pages, bool query_aware) {
+  Fp4Plan pl;
+  const int units = L->num_seqs * L->num_kv_heads, G = L->num_q_heads / L->num_kv_heads;
+  const long long frags = ((long long)pages * L->page_size + kFp4Frag - 1) / kFp4Frag * units;
+  const long long most = (frags + kFp4MinShare - 1) / kFp4MinShare;
+  pl.workgroups = most < kFp4Workgroups ? (int)most : kFp4Workgroups;
+  size_t off = kCtrlArea * sizeof(int32_t);
+  pl.off_done = off;
+  off = align_up(off + (size_t)units * sizeof(int32_t), 256);
+  pl.off_part = off;
+  off = align_up(off + (size_t)pl.workgroups * 2 * G * (L->head_dim + 2) * sizeof(float), 256);
+  pl.attend_total = off;
+  pl.off_scores = off;
+  if (query_aware) off = align_up(off + (size_t)units * L->max_pages_per_seq * sizeof(float), 256);
+  pl.off_sel = off;
+  if (query_aware) off = align_up(off + (size_t)units * pages * sizeof(int32_t), 256);
+  pl.off_count = off;
+  if (query_aware) off = align_up(off + (size_t)L->num_seqs * sizeof(int32_t), 256);
+  pl.total = off;
+  return pl;
+}
+
+static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const void* q, const int32_t* sel,
+                                const int32_t* sel_count, int Kmax, float softmax_scale, void* out, float* lse_out,
+                                unsigned char* ws, hipStream_t stream) {
+  Fp4Params p;
+  p.q = static_cast<const uint16_t*>(q);
+  p.pool = static_cast<const unsigned char*>(L->k_pool);
+  p.block_table = L->block_table;
+  p.seq_lens = L->seq_lens;
+  p.sel = sel;
+  p.sel_count = sel_count;
+  p.out = static_cast<float*>(out);
+  p.lse = lse_out;
+  p.part = reinterpret_cast<float*>(ws + pl.off_part);
+  p.done = reinterpret_cast<int32_t*>(ws + pl.off_done);
+  p.B = L->num_seqs;
+  p.Hq = L->num_q_heads;
+  p.Hkv = L->num_kv_heads;
+  p.G = p.Hq / p.Hkv;
+  p.Pmax = L->max_pages_per_seq;
+  p.Kmax = Kmax;
+  p.n_phys = L->num_phys_pages;
+  p.out_bf16 = L->out_format == TS_OUT_BF16;
+  p.tile_stride = tile_stride_of(L);
+  p.scale_log2 = softmax_scale * 1.4426950408889634f;
+  const size_t lds = kFp4List * sizeof(Fp4Entry) + (size_t)kFp4Waves * p.G * (L->head_dim + 4) * sizeof(float);
+  int st = TS_OK;
+#define TS_LAUNCH_FP4(DD, SS, SPARSE)                                              \
+  do {                                                                             \
+    if ((st = allow_lds(fp4_attention_kernel<DD, SS, SPARSE>, lds)) != TS_OK) return st; \
+    fp4_attention_kernel<DD, SS, SPARSE><<<pl.workgroups, kFp4Threads, lds, stream>>>(p); \
+  } while (0)
+#define TS_LAUNCH_FP4_LIST(DD, SS)                      \
+  do {                                                  \
+    if (sel) TS_LAUNCH_FP4(DD, SS, true);               \
+    else TS_LAUNCH_FP4(DD, SS, false);                  \
+  } while (0)
+#define TS_LAUNCH_FP4_PAGE(DD)                                  \
+  do {                                                          \
+    if (L->page_size == 8) TS_LAUNCH_FP4_LIST(DD, 8);           \
+    else if (L->page_size == 16) TS_LAUNCH_FP4_LIST(DD, 16);    \
+    else if (L->page_size == 32) TS_LAUNCH_FP4_LIST(DD, 32);    \
+    else TS_LAUNCH_FP4_LIST(DD, 64);                            \
+  } while (0)
+  if (L->head_dim == 64) TS_LAUNCH_FP4_PAGE(64);
+  else TS_LAUNCH_FP4_PAGE(128);
+#undef TS_LAUNCH_FP4_PAGE
+#undef TS_LAUNCH_FP4_LIST
+#undef TS_LAUNCH_FP4
+  return launch_status();
+}
+
+// ---------------------------------------------------------------------------
+// Rows of queries and keys
+// ---------------------------------------------------------------------------
+static bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+static int check_rotary(const ts_rotary* r, int head_dim, bool needs_positions) {
+  if (r->rot_dim < 0 || r->rot_dim > head_dim || r->rot_dim % 8 != 0) return TS_ERR_SHAPE;
+  if (!aligned(r->q_norm, 16) || !aligned(r->k_norm, 16) || !(r->norm_eps >= 0.f)) return TS_ERR_SHAPE;
+  if (r->rot_dim == 0) return TS_OK;
+  if (r->num_axes < 1 || r->num_positions < 1) return TS_ERR_SHAPE;
+  if (r->num_axes > TS_MAX_AXES) return TS_ERR_UNSUPPORTED;
+  if (!r->cos_sin || (!r->positions && (needs_positions || r->num_axes > 1))) return TS_ERR_NULL;
+  if (!aligned(r->cos_sin, 16)) return TS_ERR_SHAPE;
+  if (r->num_axes > 1)
+    for (int i = 0; i < r->rot_dim / 2; ++i)
+      if (r->axis_of_pair[i] >= r->num_axes) return TS_ERR_SHAPE;
+  return TS_OK;
+}
+
+// One of the five arrays of rows (NULL: absent).
+static int check_rows(const void* p, int64_t stride, int heads, int head_dim, int tokens) {
+  if (!p) return TS_OK;
+  if (!aligned(p, 8) || stride % 4 != 0) return TS_ERR_SHAPE;
+  if (tokens > 1 && stride < (int64_t)heads * head_dim) return TS_ERR_SHAPE;
+  return TS_OK;
+}
+
+static RotaryParams rotary_params(const ts_rotary* r, int tokens) {
+  RotaryParams p;
+  memset(&p, 0, sizeof(p));
+  p.T = tokens;
+  p.axes = 1;
+  if (!r) return p;
+  p.q_norm = r->q_norm;
+  p.k_norm = r->k_norm;
+  p.eps = r->norm_eps;
+  p.rot = r->rot_dim;
+  if (r->rot_dim == 0) return p;
+  p.table = r->cos_sin;
+  p.positions = r->positions;
+  p.adjacent = r->interleaved != 0;
+  p.axes = r->num_axes;
+  p.n_pos = r->num_positions;
+  if (r->num_axes > 1)
+    for (int i = 0; i < r->rot_dim / 2; ++i) p.axis_bits[i / 16] |= (uint32_t)r->axis_of_pair[i] << (2 * (i % 16));
+  return p;
+}
+
+static int launch_append_rows(const ts_layout* L, const ts_rotary* rotary, const ts_rows* rows, const int32_t* cu,
+                              int lens, bool store, bool table_decides, hipStream_t stream) {
+  AppendParams p;
+  p.r = rotary_params(rotary, rows->num_tokens);
+  p.q = static_cast<const uint16_t*>(rows->q);
+  p.k = static_cast<const uint16_t*>(rows->k);
+  p.v = static_cast<const uint16_t*>(rows->v);
+  p.q_out = static_cast<uint16_t*>(rows->q_out);
+  p.q_stride = rows->q_stride;
+  p.k_stride = rows->k_stride;
+  p.v_stride = rows->v_stride;
+  p.q_out_stride = rows->q_out_stride;
+  p.cu = cu;
+  p.seq_lens = L->seq_lens;
+  p.block_table = L->block_table;
+  p.k_pool = static_cast<unsigned char*>(L->k_pool);
+  p.v_pool = !store ? nullptr : static_cast<unsigned char*>(L->kv_format == TS_KV_FP4 ? L->k_pool : L->v_pool);
+  p.k_scale = L->k_scale;
+  p.v_scale = L->v_scale;
+  p.page_min = static_cast<uint16_t*>(L->page_min);
+  p.page_max = static_cast<uint16_t*>(L->page_max);
+  p.T = rows->num_tokens;
+  p.B = L->num_seqs;
+  p.Hq = L->num_q_heads;
+  p.Hkv = L->num_kv_heads;
+  p.G = p.Hq / p.Hkv;
+  p.S = L->page_size;
+  p.Pmax = L->max_pages_per_seq;
+  p.n_phys = L->num_phys_pages;
+  const bool wide = L->kv_format == TS_KV_BF16 || L->kv_format == TS_KV_FP16;
+  p.tile_stride = (long long)tile_stride_of(L) * (wide ? 2 : 1);
+  p.lens_after = lens == TS_LENS_AFTER;
+  // pages that n tokens touch: at most (n - 1) / S + 2
+  const long long pages = cu ? (long long)p.T / p.S + 2LL * p.B : p.B;
+  const dim3 grid((unsigned)pages, (unsigned)p.Hkv);
+  int st = TS_OK;
+#define TS_LAUNCH_APPEND(FMT, DD)                                                     \
+  do {                                                                                \
+    const size_t lds = AppendLds<FMT, DD>::bytes(p.S);                                \
+    if ((st = allow_lds(append_rows_kernel<FMT, DD>, lds)) != TS_OK) return st;       \
+    append_rows_kernel<FMT, DD><<<grid, kRotaryThreads, lds, stream>>>(p);            \
+  } while (0)
+#define TS_LAUNCH_APPEND_FORMAT(DD)                                                   \
+  do {                                                                                \
+    if (L->kv_format == TS_KV_FP4) TS_LAUNCH_APPEND(kPoolFp4, DD);                    \
+    else if (L->kv_format == TS_KV_INT8) TS_LAUNCH_APPEND(kPoolInt8, DD);             \
+    else if (L->kv_format == TS_KV_FP16) TS_LAUNCH_APPEND(kPoolFp16, DD);             \
+    else TS_LAUNCH_APPEND(kPoolBf16, DD);                                             \
+  } while (0)
+  if (L->head_dim == 64) TS_LAUNCH_APPEND_FORMAT(64);
+  else TS_LAUNCH_APPEND_FORMAT(128);
+#undef TS_LAUNCH_APPEND_FORMAT
+#undef TS_LAUNCH_APPEND
+  if ((st = launch_status()) != TS_OK || lens != TS_LENS_ADVANCE) return st;
+  advance_lens_kernel<<<(unsigned)((p.B + 255) / 256), 256, 0, stream>>>(
+      L->seq_lens, cu, table_decides ? L->block_table : nullptr, p.B, p.T, __builtin_ctz(p.S), p.Pmax, p.n_phys);
+  return launch_status();
+}
+
+// One token a sequence, as it is, into the 4-bit cache.
+static int append_fp4_token(const ts_layout* L, const void* k_new, const void* v_new, int advance, hipStream_t stream) {
+  ts_rows rows;
+  memset(&rows, 0, sizeof(rows));
+  rows.num_tokens = L->num_seqs;
+  rows.k = k_new;
+  rows.v = v_new;
+  rows.k_stride = rows.v_stride = (int64_t)L->num_kv_heads * L->head_dim;
+  return launch_append_rows(L, nullptr, &rows, nullptr, advance ? TS_LENS_ADVANCE : TS_LENS_KEEP, v_new != nullptr,
+                            v_new != nullptr, stream);
+}
+
 }  // namespace ts
 
 using namespace ts;
+
+// Algorithm 1 over the 4-bit cache, launch by launch.
+static int launch_fp4_query_aware(const ts_layout* layout, const void* k_new, const void* v_new, const void* q,
+                                  int32_t topk, const int32_t* topk_per_seq, int32_t max_topk, float softmax_scale,
+                                  void* out, float* scores_out, int32_t* sel_out, int32_t* sel_count_out,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  const Fp4Plan pl = make_fp4_plan(layout, max_topk, true);
+  if (workspace_bytes < pl.total) return TS_ERR_WORKSPACE;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  float* scores = scores_out ? scores_out : reinterpret_cast<float*>(ws + pl.off_scores);
+  int32_t* sel = sel_out ? sel_out : reinterpret_cast<int32_t*>(ws + pl.off_sel);
+  int32_t* count = sel_count_out ? sel_count_out : reinterpret_cast<int32_t*>(ws + pl.off_count);
+  int st = k_new ? append_fp4_token(layout, k_new, v_new, 1, (hipStream_t)stream) : TS_OK;
+  if (st == TS_OK) st = ts_score_pages(layout, q, scores, stream);
+  if (st == TS_OK) st = ts_select_topk_pages(layout, scores, topk, topk_per_seq, max_topk, sel, count, stream);
+  if (st != TS_OK) return st;
+  return launch_fp4_attention(layout, pl, q, sel, count, max_topk, softmax_scale, out, nullptr, ws, (hipStream_t)stream);
+}
 
 static int launch_fused(const ts_layout* layout, const void* k_new, const void* v_new,
                         const void* q, int32_t topk, const int32_t* topk_per_seq,
@@ -372,6 +606,9 @@ static int launch_fused(const ts_layout* layout, const void* k_new, const void* 
   if (!q || !out || !workspace || !layout->page_min || !layout->page_max) return TS_ERR_NULL;
   if ((st = check_pool(layout)) != TS_OK) return st;
   if (max_topk < 1 || (!topk_per_seq && (topk < 1 || max_topk < topk))) return TS_ERR_SHAPE;
+  if (layout->kv_format == TS_KV_FP4)
+    return launch_fp4_query_aware(layout, k_new, v_new, q, topk, topk_per_seq, max_topk, softmax_scale, out, scores_out,
+                                  sel_out, sel_count_out, workspace, workspace_bytes, stream);
   Plan pl = make_plan(layout, max_topk);
   // (a workspace without room for the partials of shares gets clusters of one size)
   if (workspace_bytes < pl.total)
@@ -419,7 +656,7 @@ static int launch_fused(const ts_layout* layout, const void* k_new, const void* 
 
 extern "C" {
 
-int ts_version(void) { return 4; }
+int ts_version(void) { return 5; }
 
 #ifdef TS_PROFILE
 // buf: device, uint64 [workgroups of the largest launch][64] (NULL: stop recording).
@@ -458,6 +695,7 @@ int ts_set_tuning(int32_t reserved, int32_t num_splits, int32_t workgroups_per_c
 
 size_t ts_workspace_bytes(const ts_layout* layout, int32_t max_topk) {
   if (check_layout(layout) != TS_OK || max_topk < 1) return 0;
+  if (layout->kv_format == TS_KV_FP4) return make_fp4_plan(layout, max_topk, true).total;
   return make_plan(layout, max_topk).total;
 }
 
@@ -497,15 +735,20 @@ int ts_build_page_meta(const ts_layout* layout, void* stream) {
     return TS_ERR_NULL;
   MetaParams p = meta_params(layout);
   if (p.B > 65535) return TS_ERR_UNSUPPORTED;
-  const bool int8 = layout->kv_format == TS_KV_INT8;
+  const bool int8 = layout->kv_format == TS_KV_INT8, fp4 = layout->kv_format == TS_KV_FP4;
   if (int8 && !layout->k_scale) return TS_ERR_NULL;
-  const int pages_per_wg = kWaves * (int8 ? 8 : kWave / (layout->head_dim / 8));
+  const int pages_per_wg = kWaves * (int8 ? 8 : kWave / (layout->head_dim / (fp4 ? 32 : 8)));
   // (the KV head is the fastest grid index: a physical page's tiles of all heads are
   // contiguous in the pool, and workgroups dispatched together then read neighbouring
   // memory: -3 % on the 16-head batch)
   if ((p.Pmax + pages_per_wg - 1) / pages_per_wg > 65535) return TS_ERR_UNSUPPORTED;
   dim3 grid(p.Hkv, (p.Pmax + pages_per_wg - 1) / pages_per_wg, p.B);
   hipStream_t s = (hipStream_t)stream;
+  if (fp4) {
+    if (layout->head_dim == 64) build_page_meta_fp4_kernel<64><<<grid, kThreads, 0, s>>>(p);
+    else build_page_meta_fp4_kernel<128><<<grid, kThreads, 0, s>>>(p);
+    return launch_status();
+  }
   if (int8) {   // (128 bytes of a page per load; up to eight loads in flight)
 #define TS_LAUNCH_BUILD8(DD, NN) build_page_meta_i8_kernel<DD, NN><<<grid, kThreads, 0, s>>>(p)
     const int loads = p.S * layout->head_dim / 128;
@@ -547,6 +790,10 @@ int ts_append_token_meta(const ts_layout* layout, const void* k_new, const void*
   int st = check_layout(layout);
   if (st != TS_OK) return st;
   if (!k_new || !layout->seq_lens || !layout->page_min || !layout->page_max) return TS_ERR_NULL;
+  if (layout->kv_format == TS_KV_FP4) {
+    if (!layout->block_table || (v_new && !layout->k_pool)) return TS_ERR_NULL;
+    return append_fp4_token(layout, k_new, v_new, advance_seq_lens, (hipStream_t)stream);
+  }
   if (v_new && (!layout->k_pool || !layout->v_pool || !layout->block_table)) return TS_ERR_NULL;
   MetaParams p = meta_params(layout);
   if (layout->kv_format == TS_KV_INT8) {
@@ -565,6 +812,69 @@ int ts_append_token_meta(const ts_layout* layout, const void* k_new, const void*
         p, layout->head_dim, static_cast<const uint16_t*>(k_new),
         static_cast<const uint16_t*>(v_new), advance_seq_lens);
   return launch_status();
+}
+
+int ts_rotate_rows(const ts_rotary* rotary, const ts_rows* rows, int32_t num_q_heads, int32_t num_kv_heads,
+                   int32_t head_dim, void* stream) {
+  if (!rotary || !rows) return TS_ERR_NULL;
+  if (rows->num_tokens < 0 || head_dim <= 0 || (rows->q && num_q_heads <= 0) || (rows->k && num_kv_heads <= 0))
+    return TS_ERR_SHAPE;
+  if (head_dim != 64 && head_dim != 128) return TS_ERR_UNSUPPORTED;
+  if (rows->format != TS_KV_BF16 && rows->format != TS_KV_FP16) return TS_ERR_UNSUPPORTED;
+  if ((!rows->q && !rows->k) || (rows->q && !rows->q_out) || (rows->k && !rows->k_out)) return TS_ERR_NULL;
+  int st = check_rotary(rotary, head_dim, rows->num_tokens > 0);
+  if (st != TS_OK) return st;
+  const int Hq = rows->q ? num_q_heads : 0, Hkv = rows->k ? num_kv_heads : 0, T = rows->num_tokens;
+  if ((long long)Hq + Hkv > (1 << 20)) return TS_ERR_UNSUPPORTED;
+  if ((st = check_rows(rows->q, rows->q_stride, Hq, head_dim, T)) != TS_OK ||
+      (st = check_rows(rows->q ? rows->q_out : nullptr, rows->q_out_stride, Hq, head_dim, T)) != TS_OK ||
+      (st = check_rows(rows->k, rows->k_stride, Hkv, head_dim, T)) != TS_OK ||
+      (st = check_rows(rows->k ? rows->k_out : nullptr, rows->k_out_stride, Hkv, head_dim, T)) != TS_OK)
+    return st;
+  if (T == 0) return TS_OK;
+  RotateParams p;
+  p.r = rotary_params(rotary, T);
+  p.q = static_cast<const uint16_t*>(rows->q);
+  p.k = static_cast<const uint16_t*>(rows->k);
+  p.q_out = static_cast<uint16_t*>(rows->q_out);
+  p.k_out = static_cast<uint16_t*>(rows->k_out);
+  p.q_stride = rows->q_stride;
+  p.k_stride = rows->k_stride;
+  p.q_out_stride = rows->q_out_stride;
+  p.k_out_stride = rows->k_out_stride;
+  p.Hq = Hq;
+  p.Hkv = Hkv;
+  p.T = T;
+  p.tokens_per_wg = 1;
+  p.rows_per_wg = Hq + Hkv;
+  const dim3 grid((unsigned)T, 1);
+  const bool half = rows->format == TS_KV_FP16;
+  hipStream_t s = (hipStream_t)stream;
+  if (head_dim == 64 && !half) rotate_rows_kernel<64, false><<<grid, kRotaryThreads, 0, s>>>(p);
+  else if (head_dim == 64) rotate_rows_kernel<64, true><<<grid, kRotaryThreads, 0, s>>>(p);
+  else if (!half) rotate_rows_kernel<128, false><<<grid, kRotaryThreads, 0, s>>>(p);
+  else rotate_rows_kernel<128, true><<<grid, kRotaryThreads, 0, s>>>(p);
+  return launch_status();
+}
+
+int ts_append_rows(const ts_layout* layout, const ts_rotary* rotary, const ts_rows* rows, const int32_t* cu_tokens,
+                   int32_t lens, void* stream) {
+  int st = check_layout(layout);
+  if (st != TS_OK) return st;
+  if (!rows || !rows->k || !rows->v || (rows->q && !rows->q_out) || !layout->page_min || !layout->page_max)
+    return TS_ERR_NULL;
+  if ((st = check_pool(layout)) != TS_OK) return st;
+  if (lens != TS_LENS_KEEP && lens != TS_LENS_ADVANCE && lens != TS_LENS_AFTER) return TS_ERR_SHAPE;
+  const int T = rows->num_tokens, d = layout->head_dim;
+  if (T < 0 || (!cu_tokens && T != layout->num_seqs)) return TS_ERR_SHAPE;
+  if (rotary && (st = check_rotary(rotary, d, false)) != TS_OK) return st;
+  if ((st = check_rows(rows->q, rows->q_stride, layout->num_q_heads, d, T)) != TS_OK ||
+      (st = check_rows(rows->q ? rows->q_out : nullptr, rows->q_out_stride, layout->num_q_heads, d, T)) != TS_OK ||
+      (st = check_rows(rows->k, rows->k_stride, layout->num_kv_heads, d, T)) != TS_OK ||
+      (st = check_rows(rows->v, rows->v_stride, layout->num_kv_heads, d, T)) != TS_OK)
+    return st;
+  if (T == 0) return TS_OK;
+  return launch_append_rows(layout, rotary, rows, cu_tokens, lens, true, false, (hipStream_t)stream);
 }
 
 int ts_score_pages(const ts_layout* layout, const void* q, float* scores, void* stream) {
@@ -646,6 +956,12 @@ int ts_sparse_decode_attention(const ts_layout* layout, const void* q, const int
   if (!q || !sel || !sel_count || !out || !workspace) return TS_ERR_NULL;
   if ((st = check_pool(layout)) != TS_OK) return st;
   if (max_topk < 1) return TS_ERR_SHAPE;
+  if (layout->kv_format == TS_KV_FP4) {
+    const Fp4Plan f = make_fp4_plan(layout, max_topk, true);
+    if (workspace_bytes < f.attend_total) return TS_ERR_WORKSPACE;
+    return launch_fp4_attention(layout, f, q, sel, sel_count, max_topk, softmax_scale, out, lse_out,
+                                static_cast<unsigned char*>(workspace), (hipStream_t)stream);
+  }
   // (clusters of one size: this call has no use for the exchange area of the fused ones)
   const Plan pl = make_plan(layout, max_topk, kTargetWorkgroups, false);
   if (workspace_bytes < pl.total) return TS_ERR_WORKSPACE;
@@ -655,6 +971,7 @@ int ts_sparse_decode_attention(const ts_layout* layout, const void* q, const int
 
 size_t ts_dense_workspace_bytes(const ts_layout* layout) {
   if (check_layout(layout) != TS_OK) return 0;
+  if (layout->kv_format == TS_KV_FP4) return make_fp4_plan(layout, layout->max_pages_per_seq, false).total;
   return make_plan(layout, layout->max_pages_per_seq, kDenseTargetWorkgroups).total;
 }
 
@@ -665,6 +982,12 @@ int ts_dense_decode_attention(const ts_layout* layout, const void* q, float soft
   if (st != TS_OK) return st;
   if (!q || !out || !workspace) return TS_ERR_NULL;
   if ((st = check_pool(layout)) != TS_OK) return st;
+  if (layout->kv_format == TS_KV_FP4) {
+    const Fp4Plan f = make_fp4_plan(layout, layout->max_pages_per_seq, false);
+    if (workspace_bytes < f.total) return TS_ERR_WORKSPACE;
+    return launch_fp4_attention(layout, f, q, nullptr, nullptr, 0, softmax_scale, out, lse_out,
+                                static_cast<unsigned char*>(workspace), (hipStream_t)stream);
+  }
   const Plan pl = make_plan(layout, layout->max_pages_per_seq, kDenseTargetWorkgroups);
   if (workspace_bytes < pl.total) return TS_ERR_WORKSPACE;
   return launch_attention(layout, pl, q, nullptr, nullptr, layout->max_pages_per_seq, softmax_scale,
@@ -675,6 +998,7 @@ int ts_append_and_decode_launches(const ts_layout* layout, int32_t max_topk) {
   const int st = check_layout(layout);
   if (st != TS_OK) return st;
   if (max_topk < 1) return TS_ERR_SHAPE;
+  if (layout->kv_format == TS_KV_FP4) return num_compute_units() <= 0 ? TS_ERR_DEVICE : 5;
   const Plan pl = make_plan(layout, max_topk);
   const int cus = num_compute_units();
   if (cus <= 0) return TS_ERR_DEVICE;
@@ -735,6 +1059,8 @@ int ts_query_aware_decode_static(const ts_layout* layout, const void* q, int32_t
   const int st = check_layout(layout);
   if (st != TS_OK) return st;
   if (max_topk < 1) return TS_ERR_SHAPE;
+  // (its partial results would lie where the other formats' launch tags do)
+  if (layout->kv_format == TS_KV_FP4) return TS_ERR_UNSUPPORTED;
   if (make_plan(layout, max_topk, kTargetWorkgroups, false).total > (size_t)TS_STATIC_WORKSPACE_BYTES)
     return TS_ERR_WORKSPACE;
   void* ws = nullptr;

@@ -1,0 +1,195 @@
+// Per-head norm and position rotation of rows of queries and keys.
+//
+// A row is one head of one token, D 16-bit numbers.  Its D / 8 lanes hold eight channels each, as two
+// chunks of four whose places depend on how the channels are paired, so that both numbers of a pair lie in
+// the same lane and nothing crosses lanes but the sum of squares:
+//   halves:    lane i < rot / 8 holds channels 4i .. 4i + 3 and rot / 2 + 4i .. + 3,
+//   adjacent:  lane i holds 8i .. 8i + 7;  lanes behind rot / 8 hold 8i .. 8i + 7 and pass them through.
+// Either way a lane's four pairs are 4i .. 4i + 3 of the rotation's rot / 2.
+//
+//   y = x * (1 / sqrt(mean x^2 + eps)) * w;   a' = a cos - b sin,  b' = b cos + a sin
+//
+// The sum of squares and its root are taken in fp64: the squares of 16-bit numbers are exact there and sums
+// of up to 128 of them all but exact, so the factor does not depend on the order of the additions.  The
+// rest is fp32, every product and sum rounded by itself (no contraction), and the row is rounded to 16 bits
+// once, at the end.  So a row has the same bits whatever kernel works it out, and what the append kernels
+// quantise is what rotate_rows_kernel would have written.
+#pragma once
+#include "ts_device.h"
+
+namespace ts {
+
+constexpr int kRotaryThreads = 256;
+constexpr int kMaxAxes = 4;
+
+struct RotaryParams {
+  const float* table;         // [n_pos][rot]: rot / 2 cosines, rot / 2 sines (null: no rotation)
+  const int32_t* positions;   // [axes][T] (null: the place in the sequence)
+  const float* q_norm;        // [D] (null: no norm)
+  const float* k_norm;
+  int rot, adjacent, axes, n_pos, T;
+  float eps;
+  uint32_t axis_bits[4];      // two bits a pair: the axis it turns by
+};
+
+template <int N>
+__device__ __forceinline__ float group_max_f32(float v) {
+  static_assert(N == 8 || N == 16, "group of 8 or 16 lanes");
+  auto take = [](float x, float y) { return fmaxf(x, y); };
+  auto move = [](float x, auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  if (N == 16) v = take(v, move(v, std::integral_constant<int, kDppMirror>{}));
+  v = take(v, move(v, std::integral_constant<int, kDppHalfMirror>{}));
+  v = take(v, move(v, std::integral_constant<int, kDppXor2>{}));
+  v = take(v, move(v, std::integral_constant<int, kDppXor1>{}));
+  return v;
+}
+
+// Where a lane's channels lie in a row, and the angles of its pairs for one token.
+template <int D>
+struct RowLanes {
+  static constexpr int kLanes = D / 8;
+  int c0, c1;     // first channel of either chunk of four
+  bool turns;
+  __device__ __forceinline__ RowLanes(const RotaryParams& p, int lane_in_row) {
+    turns = lane_in_row < p.rot / 8;
+    const bool halves = turns && !p.adjacent;
+    c0 = halves ? 4 * lane_in_row : 8 * lane_in_row;
+    c1 = halves ? p.rot / 2 + 4 * lane_in_row : 8 * lane_in_row + 4;
+  }
+};
+
+struct Angles {
+  float c[4], s[4];
+};
+
+// position_of(axis): the token's position on an axis.  Rows of the table are never read past its ends.
+template <typename PositionOf>
+__device__ __forceinline__ void load_angles(const RotaryParams& p, int lane_in_row, bool turns,
+                                            PositionOf position_of, Angles& a) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { a.c[i] = 1.f; a.s[i] = 0.f; }
+  if (!turns) return;
+  const int pair = 4 * lane_in_row, half = p.rot / 2;
+  if (p.axes == 1) {
+    const int pos = min(max(position_of(0), 0), p.n_pos - 1);
+    const float* row = p.table + (size_t)pos * p.rot + pair;
+    const float4 c = *reinterpret_cast<const float4*>(row), s = *reinterpret_cast<const float4*>(row + half);
+    a.c[0] = c.x; a.c[1] = c.y; a.c[2] = c.z; a.c[3] = c.w;
+    a.s[0] = s.x; a.s[1] = s.y; a.s[2] = s.z; a.s[3] = s.w;
+    return;
+  }
+  const uint32_t w = p.axis_bits[0] * (pair < 16) + p.axis_bits[1] * (pair >= 16 && pair < 32) +
+                     p.axis_bits[2] * (pair >= 32 && pair < 48) + p.axis_bits[3] * (pair >= 48);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int axis = (w >> (2 * ((pair + i) & 15))) & 3;
+    const int pos = min(max(position_of(axis), 0), p.n_pos - 1);
+    const float* row = p.table + (size_t)pos * p.rot + pair + i;
+    a.c[i] = row[0];
+    a.s[i] = row[half];
+  }
+}
+
+struct Norm {
+  float w[8];
+  bool on;
+};
+
+__device__ __forceinline__ void load_norm(const float* w, int c0, int c1, Norm& n) {
+  n.on = w != nullptr;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) n.w[i] = 1.f;
+  if (!n.on) return;
+  const float4 a = *reinterpret_cast<const float4*>(w + c0), b = *reinterpret_cast<const float4*>(w + c1);
+  n.w[0] = a.x; n.w[1] = a.y; n.w[2] = a.z; n.w[3] = a.w;
+  n.w[4] = b.x; n.w[5] = b.y; n.w[6] = b.z; n.w[7] = b.w;
+}
+
+template <bool kHalf>
+__device__ __forceinline__ uint32_t pack_elems(float x, float y) {
+  if (kHalf) return (uint32_t)f32_to_half(x) | (uint32_t)f32_to_half(y) << 16;
+  return (uint32_t)f32_to_bf16_rn(x) | (uint32_t)f32_to_bf16_rn(y) << 16;
+}
+
+// One row, eight channels a lane: normed, rotated and rounded to 16 bits.  All lanes of the row take part.
+template <int D, bool kHalf>
+__device__ __forceinline__ void rotate_row(const RotaryParams& p, bool turns, const Norm& n, const Angles& t,
+                                           uint2& a, uint2& b) {
+#pragma clang fp contract(off)
+  float y[8] = {elem_lo<kHalf>(a.x), elem_hi<kHalf>(a.x), elem_lo<kHalf>(a.y), elem_hi<kHalf>(a.y),
+                elem_lo<kHalf>(b.x), elem_hi<kHalf>(b.x), elem_lo<kHalf>(b.y), elem_hi<kHalf>(b.y)};
+  if (n.on) {
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = fma((double)y[i], (double)y[i], sum);
+    sum = group_sum1_f64<D / 8>(sum);
+    const float r = (float)(1.0 / sqrt(sum * (1.0 / D) + (double)p.eps));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (y[i] * r) * n.w[i];
+  }
+  if (turns) {
+    float z[8];
+    if (p.adjacent) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        z[2 * i] = y[2 * i] * t.c[i] - y[2 * i + 1] * t.s[i];
+        z[2 * i + 1] = y[2 * i + 1] * t.c[i] + y[2 * i] * t.s[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        z[i] = y[i] * t.c[i] - y[4 + i] * t.s[i];
+        z[4 + i] = y[4 + i] * t.c[i] + y[i] * t.s[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = z[i];
+  }
+  if (n.on || turns) {   // (what neither norm nor rotation touches keeps its bits)
+    a = make_uint2(pack_elems<kHalf>(y[0], y[1]), pack_elems<kHalf>(y[2], y[3]));
+    b = make_uint2(pack_elems<kHalf>(y[4], y[5]), pack_elems<kHalf>(y[6], y[7]));
+  }
+}
+
+struct RotateParams {
+  RotaryParams r;
+  const uint16_t *q, *k;         // either may be null
+  uint16_t *q_out, *k_out;
+  long long q_stride, k_stride, q_out_stride, k_out_stride;   // elements between tokens
+  int Hq, Hkv, T;
+  int tokens_per_wg, rows_per_wg;   // a workgroup's tokens (a power of two) and heads
+};
+
+// grid (tokens / tokens_per_wg, heads / rows_per_wg).  A row's lanes stay with their token, whose angles
+// they hold, and take its heads in turn.  Memory-bound: every element is read and written once.
+template <int D, bool kHalf>
+__global__ __launch_bounds__(kRotaryThreads) void rotate_rows_kernel(RotateParams p) {
+  constexpr int LPR = D / 8, NG = kRotaryThreads / LPR;
+  const int group = threadIdx.x / LPR, li = threadIdx.x % LPR;
+  const int t = blockIdx.x * p.tokens_per_wg + group % p.tokens_per_wg, step = NG / p.tokens_per_wg;
+  const bool on = t < p.T;
+  const int tc = on ? t : p.T - 1;
+  const RowLanes<D> lanes(p.r, li);
+  Angles ang;
+  load_angles(p.r, li, lanes.turns, [&](int axis) { return p.r.positions[(size_t)axis * p.r.T + tc]; }, ang);
+  Norm qn, kn;
+  load_norm(p.r.q_norm, lanes.c0, lanes.c1, qn);
+  load_norm(p.r.k_norm, lanes.c0, lanes.c1, kn);
+  const int rows = p.Hq + p.Hkv, end = min(rows, (int)(blockIdx.y + 1) * p.rows_per_wg);
+  for (int row = blockIdx.y * p.rows_per_wg + group / p.tokens_per_wg; row < end; row += step) {
+    const bool is_q = row < p.Hq;
+    const uint16_t* src = is_q ? p.q + tc * p.q_stride + row * D : p.k + tc * p.k_stride + (row - p.Hq) * D;
+    uint16_t* dst = is_q ? p.q_out + tc * p.q_out_stride + row * D : p.k_out + tc * p.k_out_stride + (row - p.Hq) * D;
+    uint2 a = *reinterpret_cast<const uint2*>(src + lanes.c0), b = *reinterpret_cast<const uint2*>(src + lanes.c1);
+    if (is_q) rotate_row<D, kHalf>(p.r, lanes.turns, qn, ang, a, b);
+    else rotate_row<D, kHalf>(p.r, lanes.turns, kn, ang, a, b);
+    if (on) {
+      *reinterpret_cast<uint2*>(dst + lanes.c0) = a;
+      *reinterpret_cast<uint2*>(dst + lanes.c1) = b;
+    }
+  }
+}
+
+}  // namespace ts

@@ -27,13 +27,18 @@ TS_OUT_BF16 = 1
 TS_KV_BF16 = 0
 TS_KV_INT8 = 1
 TS_KV_FP16 = 2
+TS_KV_FP4 = 3
+TS_LENS_KEEP = 0
+TS_LENS_ADVANCE = 1
+TS_LENS_AFTER = 2
+MAX_AXES = 4
 
 EXPORTS = [
     "ts_build_page_meta", "ts_append_token_meta", "ts_score_pages", "ts_select_topk_pages",
     "ts_sparse_decode_attention", "ts_query_aware_decode", "ts_append_and_decode",
     "ts_append_and_decode_launches", "ts_dense_workspace_bytes", "ts_dense_decode_attention", "ts_workspace_bytes",
     "ts_workspace_init", "ts_workspace_status", "ts_set_tuning", "ts_strerror", "ts_version",
-    "ts_debug_xcc_ids", "ts_query_aware_decode_static",
+    "ts_debug_xcc_ids", "ts_query_aware_decode_static", "ts_rotate_rows", "ts_append_rows",
 ]
 
 
@@ -50,6 +55,26 @@ class TsLayout(ctypes.Structure):
         ("out_format", ctypes.c_int32), ("kv_format", ctypes.c_int32),
         ("cluster_size", ctypes.c_int32), ("wait_limit", ctypes.c_int32),
         ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+    ]
+
+
+class TsRotary(ctypes.Structure):
+    _fields_ = [
+        ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+        ("num_axes", ctypes.c_int32), ("num_positions", ctypes.c_int32),
+        ("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+        ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p),
+        ("norm_eps", ctypes.c_float), ("axis_of_pair", ctypes.c_uint8 * 64),
+    ]
+
+
+class TsRows(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32), ("format", ctypes.c_int32),
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+        ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64),
     ]
 
 
@@ -89,6 +114,8 @@ def lib():
         L.ts_workspace_bytes.restype = sz
         L.ts_workspace_init.argtypes = [vp, sz, vp]
         L.ts_workspace_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32)]
+        L.ts_rotate_rows.argtypes = [ctypes.POINTER(TsRotary), ctypes.POINTER(TsRows), i32, i32, i32, vp]
+        L.ts_append_rows.argtypes = [lp, ctypes.POINTER(TsRotary), ctypes.POINTER(TsRows), vp, i32, vp]
         L.ts_set_tuning.argtypes = [i32, i32, i32]
         L.ts_debug_xcc_ids.argtypes = [vp, i32, vp]
         L.ts_strerror.argtypes = [ctypes.c_int]
@@ -124,14 +151,15 @@ def make_layout(B, Hq, Hkv, d, S, P_max, k_pool, v_pool, block_table, seq_lens, 
                 k_scale=None, v_scale=None, cluster_size=0, wait_limit=0) -> TsLayout:
     """Fill the C struct; tensors must stay alive while calls using it are in flight.
     int8 pools (with k_scale / v_scale) select the INT8 cache format, float16 pools the
-    FP16 one (q, new tokens and metadata must then be float16 too)."""
+    FP16 one (q, new tokens and metadata must then be float16 too), a uint8 k_pool
+    [n_phys][Hkv][S * (d + 4) bytes or more] with v_pool None the 4-bit one (new_fp4_pool)."""
     n_phys = 0 if k_pool is None else k_pool.shape[0]
     tile_stride = 0
     if k_pool is not None and Hkv > 1:
         # [n_phys][Hkv][...]: distance between the tiles of two heads (S*d for dense pools,
         # 2*S*d when the K and V tiles of a page are interleaved in one allocation)
         tile_stride = int(k_pool.stride(1))
-        assert k_pool.stride(0) == Hkv * tile_stride and v_pool.stride(1) == tile_stride
+        assert k_pool.stride(0) == Hkv * tile_stride and (v_pool is None or v_pool.stride(1) == tile_stride)
     elif k_pool is not None:
         tile_stride = int(k_pool.stride(0))
     lay = TsLayout(B, Hq, Hkv, d, S, P_max, n_phys, tile_stride,
@@ -143,11 +171,121 @@ def make_layout(B, Hq, Hkv, d, S, P_max, k_pool, v_pool, block_table, seq_lens, 
                    None if page_max is None else page_max.data_ptr(),
                    int(keep_first_pages), int(keep_last_pages), int(out_format),
                    (TS_KV_BF16 if k_pool is None else
-                    {torch.int8: TS_KV_INT8, torch.float16: TS_KV_FP16}.get(k_pool.dtype, TS_KV_BF16)),
+                    {torch.int8: TS_KV_INT8, torch.float16: TS_KV_FP16, torch.uint8: TS_KV_FP4}.get(k_pool.dtype, TS_KV_BF16)),
                    int(cluster_size), int(wait_limit),
                    None if k_scale is None else k_scale.data_ptr(),
                    None if v_scale is None else v_scale.data_ptr())
     return lay
+
+
+def fp4_block_bytes(S, d) -> int:
+    """Bytes of one (page, KV head) block of the 4-bit cache."""
+    return S * (d + 4)
+
+
+def new_fp4_pool(num_phys_pages, Hkv, S, d, device) -> torch.Tensor:
+    """An empty 4-bit cache: uint8 [num_phys_pages][Hkv][fp4_block_bytes], the k_pool of make_layout."""
+    return torch.zeros((num_phys_pages, Hkv, fp4_block_bytes(S, d)), dtype=torch.uint8, device=device)
+
+
+def rotary_table(num_positions, rot_dim, base=10000.0, device="cuda") -> torch.Tensor:
+    """cos_sin for positions 0 .. num_positions - 1 with frequencies base ** (-2 i / rot_dim), worked
+    out in 64 bits.  (Any other table, of scaled or stretched positions, serves as well.)"""
+    i = torch.arange(rot_dim // 2, dtype=torch.float64, device=device)
+    at = torch.arange(num_positions, dtype=torch.float64, device=device)[:, None] * base ** (-2.0 * i / rot_dim)
+    return torch.cat([at.cos(), at.sin()], dim=1).float().contiguous()
+
+
+def make_rotary(cos_sin=None, positions=None, interleaved=False, axis_of_pair=None, q_norm=None, k_norm=None,
+                norm_eps=1e-6) -> TsRotary:
+    """Norm and rotation of rows.  cos_sin: fp32 [num_positions][rot_dim] (None: no rotation).
+    positions: int32 [num_tokens] or [num_axes][num_tokens]; with several axes axis_of_pair says for
+    each of the rot_dim / 2 pairs which one it turns by.  q_norm, k_norm: fp32 [d] (None: no norm).
+    The tensors are held by the struct."""
+    axes = 1 if positions is None or positions.dim() == 1 else positions.shape[0]
+    rows, rot = (0, 0) if cos_sin is None else cos_sin.shape
+    for t, dtype in ((cos_sin, torch.float32), (positions, torch.int32), (q_norm, torch.float32),
+                     (k_norm, torch.float32)):
+        if t is not None and (t.dtype != dtype or not t.is_contiguous()):
+            raise TinyServeError(TS_ERR_SHAPE, "make_rotary")
+    r = TsRotary(rot, int(interleaved), axes, rows, _ptr(cos_sin), _ptr(positions), _ptr(q_norm), _ptr(k_norm),
+                 float(norm_eps))
+    if axes > 1:
+        if axis_of_pair is None or len(axis_of_pair) != rot // 2:
+            raise TinyServeError(TS_ERR_SHAPE, "make_rotary")
+        r.axis_of_pair[:rot // 2] = [int(a) for a in axis_of_pair]
+    r.held = (cos_sin, positions, q_norm, k_norm)
+    r.tokens = None if positions is None else positions.shape[-1]
+    r.norm_dim = {t.numel() for t in (q_norm, k_norm) if t is not None}
+    return r
+
+
+def _row_stride(t, like, where):
+    """Elements between the tokens of [num_tokens][heads][d]; like: a tensor of the same tokens and type."""
+    if (t.dim() != 3 or t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] > 1)
+            or t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.shape[2] != like.shape[2]):
+        raise TinyServeError(TS_ERR_SHAPE, where)
+    return t.stride(0)
+
+
+def _check_rotary(rotary, tokens, d, where):
+    if (rotary.tokens is not None and rotary.tokens != tokens) or not rotary.norm_dim <= {d}:
+        raise TinyServeError(TS_ERR_SHAPE, where)
+
+
+_ROW_FORMATS = {torch.bfloat16: TS_KV_BF16, torch.float16: TS_KV_FP16}
+
+
+def rotate_rows(rotary, q, k, q_out=None, k_out=None):
+    """Per-head norm and rotation of q [num_tokens][Hq][d] and k [num_tokens][Hkv][d] (either may be
+    None), which may be slices of one projection's rows; in place where no output is given."""
+    where = "ts_rotate_rows"
+    one = q if q is not None else k
+    if one is None or one.dtype not in _ROW_FORMATS:
+        raise TinyServeError(TS_ERR_NULL if one is None else TS_ERR_UNSUPPORTED, where)
+    q_out = q if q_out is None else q_out
+    k_out = k if k_out is None else k_out
+    n, _, d = one.shape
+    _check_rotary(rotary, n, d, where)
+    Hq = Hkv = qs = ks = qos = kos = 0
+    if q is not None:
+        Hq, qs, qos = q.shape[1], _row_stride(q, one, where), _row_stride(q_out, one, where)
+    if k is not None:
+        Hkv, ks, kos = k.shape[1], _row_stride(k, one, where), _row_stride(k_out, one, where)
+    if (Hq and q_out.shape[1] != Hq) or (Hkv and k_out.shape[1] != Hkv):
+        raise TinyServeError(TS_ERR_SHAPE, where)
+    rows = TsRows(n, _ROW_FORMATS[one.dtype], _ptr(q), _ptr(k), None, _ptr(q_out), _ptr(k_out), qs, ks, 0, qos, kos)
+    _check(lib().ts_rotate_rows(ctypes.byref(rotary), ctypes.byref(rows), Hq, Hkv, d, _stream()), where)
+
+
+def append_rows(layout, k, v, rotary=None, q=None, q_out=None, cu_tokens=None, advance_seq_lens=True,
+                lens_include_new=False):
+    """Append k, v [num_tokens][Hkv][d] to the cache, normed and rotated on the way (rotary), one token
+    for each sequence or, with cu_tokens (int32 [num_seqs + 1], on the device), any number; q
+    [num_tokens][Hq][d] is normed and rotated into q_out (in place if none is given) in the same
+    launch.  lens_include_new: the layout's lengths count the new tokens already."""
+    where = "ts_append_rows"
+    half = layout.kv_format == TS_KV_FP16
+    if k.dtype != (torch.float16 if half else torch.bfloat16):
+        raise TinyServeError(TS_ERR_UNSUPPORTED, where)
+    n, Hkv, d = k.shape
+    if rotary is not None:
+        _check_rotary(rotary, n, d, where)
+    qs = qos = 0
+    if q is not None:
+        q_out = q if q_out is None else q_out
+        qs, qos = _row_stride(q, k, where), _row_stride(q_out, k, where)
+        if q.shape[1] != layout.num_q_heads or q_out.shape[1] != layout.num_q_heads:
+            raise TinyServeError(TS_ERR_SHAPE, where)
+    ks, vs = _row_stride(k, k, where), _row_stride(v, k, where)
+    if Hkv != layout.num_kv_heads or v.shape[1] != Hkv or d != layout.head_dim or (
+            n != layout.num_seqs if cu_tokens is None else
+            cu_tokens.dtype != torch.int32 or cu_tokens.numel() != layout.num_seqs + 1):
+        raise TinyServeError(TS_ERR_SHAPE, where)
+    lens = TS_LENS_AFTER if lens_include_new else TS_LENS_ADVANCE if advance_seq_lens else TS_LENS_KEEP
+    rows = TsRows(n, 0, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out) if q is not None else None, None, qs, ks, vs, qos, 0)
+    _check(lib().ts_append_rows(ctypes.byref(layout), None if rotary is None else ctypes.byref(rotary),
+                                ctypes.byref(rows), _ptr(cu_tokens), lens, _stream()), where)
 
 
 def build_page_meta(layout):
