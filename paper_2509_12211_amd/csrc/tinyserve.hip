@@ -386,8 +386,11 @@ static Fp4Plan make_fp4_plan(const ts_layout* L, int pages, bool query_aware) {
   Fp4Plan pl;
   const int units = L->num_seqs * L->num_kv_heads, G = L->num_q_heads / L->num_kv_heads;
   const long long frags = ((long long)pages * L->page_size + kFp4Frag - 1) / kFp4Frag * units;
-  const long long most = (frags + kFp4MinShare - 1) / kFp4MinShare;
-  pl.workgroups = most < kFp4Workgroups ? (int)most : kFp4Workgroups;
+  const bool d64 = L->head_dim == 64;
+  const int share = d64 ? Fp4Shape<64>::kMinShare : Fp4Shape<128>::kMinShare;
+  const int resident = d64 ? Fp4Shape<64>::kResident : Fp4Shape<128>::kResident;
+  const long long most = (frags + share - 1) / share;
+  pl.workgroups = most < resident ? (int)most : resident;
   size_t off = kCtrlArea * sizeof(int32_t);
   pl.off_done = off;
   off = align_up(off + (size_t)units * sizeof(int32_t), 256);
@@ -428,12 +431,13 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
   p.out_bf16 = L->out_format == TS_OUT_BF16;
   p.tile_stride = tile_stride_of(L);
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
-  const size_t lds = kFp4List * sizeof(Fp4Entry) + (size_t)kFp4Waves * p.G * (L->head_dim + 4) * sizeof(float);
+  const int waves = L->head_dim == 64 ? Fp4Shape<64>::kWavesPer : Fp4Shape<128>::kWavesPer;
+  const size_t lds = kFp4List * sizeof(Fp4Entry) + (size_t)waves * p.G * (L->head_dim + 4) * sizeof(float);
   int st = TS_OK;
 #define TS_LAUNCH_FP4(DD, SS, SPARSE)                                              \
   do {                                                                             \
     if ((st = allow_lds(fp4_attention_kernel<DD, SS, SPARSE>, lds)) != TS_OK) return st; \
-    fp4_attention_kernel<DD, SS, SPARSE><<<pl.workgroups, kFp4Threads, lds, stream>>>(p); \
+    fp4_attention_kernel<DD, SS, SPARSE><<<pl.workgroups, waves * kWave, lds, stream>>>(p); \
   } while (0)
 #define TS_LAUNCH_FP4_LIST(DD, SS)                      \
   do {                                                  \
@@ -535,15 +539,20 @@ static int launch_append_rows(const ts_layout* L, const ts_rotary* rotary, const
   const bool wide = L->kv_format == TS_KV_BF16 || L->kv_format == TS_KV_FP16;
   p.tile_stride = (long long)tile_stride_of(L) * (wide ? 2 : 1);
   p.lens_after = lens == TS_LENS_AFTER;
-  // pages that n tokens touch: at most (n - 1) / S + 2
-  const long long pages = cu ? (long long)p.T / p.S + 2LL * p.B : p.B;
-  const dim3 grid((unsigned)pages, (unsigned)p.Hkv);
   int st = TS_OK;
-#define TS_LAUNCH_APPEND(FMT, DD)                                                     \
-  do {                                                                                \
-    const size_t lds = AppendLds<FMT, DD>::bytes(p.S);                                \
-    if ((st = allow_lds(append_rows_kernel<FMT, DD>, lds)) != TS_OK) return st;       \
-    append_rows_kernel<FMT, DD><<<grid, kRotaryThreads, lds, stream>>>(p);            \
+#define TS_LAUNCH_APPEND(FMT, DD)                                                             \
+  do {                                                                                        \
+    if (cu) {                                                                                 \
+      const size_t lds = AppendLds<FMT, DD>::bytes(p.S);                                      \
+      /* pages that n tokens touch: at most (n - 1) / S + 2 */                                \
+      const long long pages = (long long)p.T / p.S + 2LL * p.B;                               \
+      const dim3 grid((unsigned)pages, (unsigned)p.Hkv);                                      \
+      append_rows_kernel<FMT, DD><<<grid, kRotaryThreads, lds, stream>>>(p);                  \
+    } else {                                                                                  \
+      const int groups = kRotaryThreads / (DD / 8), n = 2 * p.Hkv + (p.q ? p.Hq : 0);         \
+      const dim3 grid((unsigned)p.B, (unsigned)((n + groups - 1) / groups));                  \
+      append_token_rows_kernel<FMT, DD><<<grid, kRotaryThreads, 0, stream>>>(p);              \
+    }                                                                                         \
   } while (0)
 #define TS_LAUNCH_APPEND_FORMAT(DD)                                                   \
   do {                                                                                \
@@ -845,9 +854,17 @@ int ts_rotate_rows(const ts_rotary* rotary, const ts_rows* rows, int32_t num_q_h
   p.Hq = Hq;
   p.Hkv = Hkv;
   p.T = T;
+  // Eight rows for each group of lanes, as long as that leaves four workgroups for every compute unit; the
+  // fewest tokens get a row for each group and as many workgroups as that takes.
+  const int groups = kRotaryThreads / (head_dim / 8), rows_all = Hq + Hkv;
   p.tokens_per_wg = 1;
-  p.rows_per_wg = Hq + Hkv;
-  const dim3 grid((unsigned)T, 1);
+  while (p.tokens_per_wg < groups && rows_all * p.tokens_per_wg < 8 * groups &&
+         T / (2 * p.tokens_per_wg) >= 4 * kTargetWorkgroups)
+    p.tokens_per_wg *= 2;
+  p.rows_per_wg = rows_all;
+  while (p.tokens_per_wg == 1 && p.rows_per_wg > groups && (long long)T * ((rows_all + p.rows_per_wg - 1) / p.rows_per_wg) < 4 * kTargetWorkgroups)
+    p.rows_per_wg = (p.rows_per_wg / 2 + groups - 1) / groups * groups;
+  const dim3 grid((unsigned)((T + p.tokens_per_wg - 1) / p.tokens_per_wg), (unsigned)((rows_all + p.rows_per_wg - 1) / p.rows_per_wg));
   const bool half = rows->format == TS_KV_FP16;
   hipStream_t s = (hipStream_t)stream;
   if (head_dim == 64 && !half) rotate_rows_kernel<64, false><<<grid, kRotaryThreads, 0, s>>>(p);

@@ -2,11 +2,13 @@
 // the way (ts_rotary.h), values transposed into their channel-major tiles, page boxes opened or widened, the
 // queries of the same tokens rotated in the same launch.
 //
-// A workgroup takes the tokens that fall into ONE page of one sequence, for one KV head and the query
-// heads that share it.  So a page's tile and its box have one writer, what the page held already needs no
-// atomics, and the box of a new page is worked out from the tokens in hand.  Keys go from registers to
-// their slots; the values, and the keys' stored form for the box, pass through LDS.
+// With offsets a workgroup takes the tokens that fall into ONE page of one sequence, for one KV head and the
+// query heads that share it.  So a page's tile and its box have one writer, what the page held already needs
+// no atomics, and the box of a new page is worked out from the tokens in hand.  Keys go from registers to
+// their slots, the values through LDS.  One token for each sequence goes row by row instead.
 #pragma once
+#include <float.h>
+
 #include "ts_meta.h"
 #include "ts_rotary.h"
 
@@ -22,21 +24,51 @@ constexpr int kPoolBf16 = 0, kPoolInt8 = 1, kPoolFp16 = 2, kPoolFp4 = 3;
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float fp4_row_scale(float amax) {
   if (!(amax > 0.f)) return 1.0f;
-  const uint32_t b = __float_as_uint(__fdiv_rn(fminf(amax, 3.3e38f), 6.0f));
+  const uint32_t b = __float_as_uint(__fdiv_rn(fminf(amax, FLT_MAX), 6.0f));
   return __uint_as_float((b + 0xffffu) & 0xffff0000u);
 }
-// Nearest code, ties to the even one; no negative zero; NaN is 0.
-__device__ __forceinline__ uint32_t fp4_code(float x, float scale) {
-  const float r = __fdiv_rn(x, scale), m = fabsf(r);
-  const uint32_t c = (uint32_t)(m > 0.25f) + (uint32_t)(m >= 0.75f) + (uint32_t)(m > 1.25f) + (uint32_t)(m >= 1.75f) +
-                     (uint32_t)(m > 2.5f) + (uint32_t)(m >= 3.5f) + (uint32_t)(m > 5.0f);
-  return c != 0u && r < 0.f ? c | 8u : c;
+typedef float float2_t __attribute__((ext_vector_type(2)));
+// The codes of eight numbers of a row, four bits each: the nearest, ties to the even code, no negative zero; NaN
+// is 0.  The quotient is the reciprocal's product corrected by its remainder: exact where x / scale is a
+// number's border (a tie), and elsewhere off by far less than the 2^-11 that eight-bit numbers keep away from
+// one.  Rows of very small or large scale are moved to the middle of the range first (exactly).
+struct Fp4Quotient {
+  float f, s, r;
+  __device__ __forceinline__ explicit Fp4Quotient(float scale) {
+    f = scale < 0x1p-60f ? 0x1p100f : scale > 0x1p60f ? 0x1p-100f : 1.0f;
+    s = scale * f;
+    r = __builtin_amdgcn_rcpf(s);
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    x *= f;
+    const float q = x * r;
+    const float z = fmaf(fmaf(-q, s, x), r, q);
+    return fminf(fmaxf(z, -6.0f), 6.0f);
+  }
+};
+__device__ __forceinline__ uint32_t fp4_codes(const float (&x)[8], float scale) {
+  const Fp4Quotient quotient(scale);
+  float z[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    // infinities saturate, NaN is 0
+    const float y = fminf(fmaxf(x[i], -FLT_MAX), FLT_MAX);
+    z[i] = x[i] == x[i] ? quotient(y) : 0.f;
+  }
+  uint32_t w = 0u;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, z[0], z[1], 1.0f, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, z[2], z[3], 1.0f, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, z[4], z[5], 1.0f, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, z[6], z[7], 1.0f, 3);
+  const uint32_t m = w & 0x77777777u;
+  return m | (w & (m + 0x77777777u) & 0x88888888u);   // signs of the numbers that are not zero
 }
-__device__ __forceinline__ float fp4_value(uint32_t code) {
-  const uint32_t m = code & 7u;
-  // twice the magnitudes, a nibble each but the last: 0 1 2 3 4 6 8 12
-  const float v = 0.5f * (float)((0xc8643210u >> (4 * m)) & 15u);
-  return (code & 8u) != 0u ? -v : v;
+// The numbers of eight codes, times a factor.
+__device__ __forceinline__ void fp4_numbers(uint32_t w, float scale, float (&x)[8]) {
+  const float2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+  const float2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+  x[0] = a[0] * scale; x[1] = a[1] * scale; x[2] = b[0] * scale; x[3] = b[1] * scale;
+  x[4] = c[0] * scale; x[5] = c[1] * scale; x[6] = d[0] * scale; x[7] = d[1] * scale;
 }
 // An exactly known fp32 value rounded to bf16 on one side of it.
 __device__ __forceinline__ uint32_t bf16_outwards(float f, bool up) {
@@ -67,7 +99,7 @@ struct AppendParams {
   const uint16_t *q, *k, *v;          // q may be null
   uint16_t* q_out;
   long long q_stride, k_stride, v_stride, q_out_stride;   // elements between tokens
-  const int32_t* cu;                  // [B + 1] first token of each sequence (null: one token each)
+  const int32_t* cu;                  // [B + 1] first token of each sequence (append_rows_kernel)
   const int32_t* seq_lens;
   const int32_t* block_table;
   unsigned char *k_pool, *v_pool;     // 4 bits: the blocks; v_pool null: boxes only
@@ -81,12 +113,209 @@ struct AppendParams {
 template <int FMT, int D>
 struct AppendLds {
   typedef typename std::conditional<FMT == kPoolInt8 || FMT == kPoolFp4, uint8_t, uint16_t>::type Elem;
-  static constexpr int kRow = D + 8;   // elements of a staged row
-  static constexpr int kParts = kRotaryThreads / D;
+  static constexpr int kRow = D + 8;   // elements of a staged row of values
+  static constexpr int kWavesPer = kRotaryThreads / kWave;
   __host__ __device__ static constexpr size_t bytes(int S) {
-    return 2 * (size_t)S * kRow * sizeof(Elem) + (size_t)S * 4 + 2 * (size_t)kParts * D * 4;
+    return (size_t)S * kRow * sizeof(Elem) + 2 * (size_t)kWavesPer * D * 4;
   }
 };
+
+// A row as the cache stores it: 16 bits (two chunks of four), eight int8 codes, or eight 4-bit codes.
+struct StoredRow {
+  uint2 a, b;
+  float scale;
+};
+template <int FMT, int D>
+__device__ __forceinline__ StoredRow store_form(uint2 x, uint2 y) {
+  StoredRow s;
+  s.a = x;
+  s.b = y;
+  s.scale = 1.f;
+  if constexpr (FMT == kPoolInt8 || FMT == kPoolFp4) {
+    const float f[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y),
+                        bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(f[i]));
+    amax = group_max_f32<D / 8>(amax);
+    if constexpr (FMT == kPoolInt8) {
+      s.scale = i8_row_scale(amax);
+      uint32_t c[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] = (uint32_t)i8_code(f[i], s.scale) & 0xffu;
+      s.a.x = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+      s.b.x = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
+    } else {
+      s.scale = fp4_row_scale(amax);
+      s.a.x = fp4_codes(f, s.scale);
+    }
+  }
+  return s;
+}
+// Its numbers as fp32, the smaller and the larger bf16 neighbour where fp32 does not hold them (INT8).
+template <int FMT>
+__device__ __forceinline__ void stored_numbers(const StoredRow& s, float (&lo)[8], float (&hi)[8]) {
+  if constexpr (FMT == kPoolFp4) {
+    fp4_numbers(s.a.x, s.scale, lo);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) hi[i] = lo[i];
+  } else if constexpr (FMT == kPoolInt8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const double x = (double)(int8_t)((i < 4 ? s.a.x : s.b.x) >> (8 * (i & 3))) * (double)s.scale;
+      lo[i] = bf16_to_f32(bf16_directed(x, false));
+      hi[i] = bf16_to_f32(bf16_directed(x, true));
+    }
+  } else {
+    constexpr bool kHalf = FMT == kPoolFp16;
+    const uint32_t w[4] = {s.a.x, s.a.y, s.b.x, s.b.y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo[2 * i] = hi[2 * i] = elem_lo<kHalf>(w[i]);
+      lo[2 * i + 1] = hi[2 * i + 1] = elem_hi<kHalf>(w[i]);
+    }
+  }
+}
+// A key's chunks (channels c0 and c1 on) into its slot of the tile, and its scale.
+template <int FMT, int D>
+__device__ __forceinline__ void store_key(const AppendParams& p, unsigned char* tile, size_t scale_row, int slot, int c0, int c1,
+                                          int li, const StoredRow& s) {
+  if constexpr (FMT == kPoolFp4) {
+    unsigned char* dst = tile + slot * (D / 2);
+    *reinterpret_cast<uint16_t*>(dst + c0 / 2) = (uint16_t)s.a.x;
+    *reinterpret_cast<uint16_t*>(dst + c1 / 2) = (uint16_t)(s.a.x >> 16);
+    if (li == 0)
+      *reinterpret_cast<uint16_t*>(tile + Fp4Block<D>::key_scales(p.S) + 2 * slot) = (uint16_t)(__float_as_uint(s.scale) >> 16);
+  } else if constexpr (FMT == kPoolInt8) {
+    *reinterpret_cast<uint32_t*>(tile + slot * D + c0) = s.a.x;
+    *reinterpret_cast<uint32_t*>(tile + slot * D + c1) = s.b.x;
+    if (li == 0) p.k_scale[scale_row + slot] = s.scale;
+  } else {
+    uint16_t* dst = reinterpret_cast<uint16_t*>(tile) + slot * D;
+    *reinterpret_cast<uint2*>(dst + c0) = s.a;
+    *reinterpret_cast<uint2*>(dst + c1) = s.b;
+  }
+}
+template <int FMT, int D>
+__device__ __forceinline__ void store_value_scale(const AppendParams& p, unsigned char* block, size_t scale_row, int slot, float scale) {
+  if constexpr (FMT == kPoolFp4)
+    *reinterpret_cast<uint16_t*>(block + Fp4Block<D>::value_scales(p.S) + 2 * slot) = (uint16_t)(__float_as_uint(scale) >> 16);
+  else if constexpr (FMT == kPoolInt8) p.v_scale[scale_row + slot] = scale;
+}
+// fp32 numbers known exactly, or (16 bits, INT8) 16-bit numbers already, as the box holds them.
+template <int FMT>
+__device__ __forceinline__ uint16_t box_number(float f, bool up) {
+  if constexpr (FMT == kPoolFp4) return (uint16_t)bf16_outwards(f, up);
+  else if constexpr (FMT == kPoolFp16) return f32_to_half(f);
+  else return (uint16_t)(__float_as_uint(f) >> 16);
+}
+// Where the page `phys` keeps the head's keys (4 bits: the block), its values and its scales.
+template <int FMT, int D>
+struct PageTiles {
+  unsigned char *k, *v;
+  size_t scale_row;
+  __device__ __forceinline__ PageTiles(const AppendParams& p, int phys, int h) {
+    const size_t id = (size_t)phys * p.Hkv + h;
+    k = p.k_pool + id * (size_t)p.tile_stride;
+    v = FMT == kPoolFp4 ? k + Fp4Block<D>::values(p.S) : p.v_pool + id * (size_t)p.tile_stride;
+    scale_row = id * (size_t)p.S;
+  }
+};
+
+// One token for each sequence: every row by itself, eight or sixteen lanes for each, no LDS and no barrier.
+// A key's lanes widen or open its page's box in the channels they hold; a value's lanes put its eight
+// numbers into their places in the channel-major tile.  Bound by a chain of trips to memory (length,
+// block-table entry and angles, box); the row itself is asked for ahead of them.
+// grid (sequences, row groups): rows 0 .. Hkv - 1 keys, then values, then queries.
+template <int FMT, int D>
+__global__ __launch_bounds__(kRotaryThreads) void append_token_rows_kernel(AppendParams p) {
+  constexpr bool kHalf = FMT == kPoolFp16;
+  constexpr int LPR = D / 8, NG = kRotaryThreads / LPR;
+  const int b = blockIdx.x, li = threadIdx.x % LPR, row = blockIdx.y * NG + threadIdx.x / LPR;
+  const int rows = 2 * p.Hkv + (p.q != nullptr ? p.Hq : 0);
+  if (row >= rows) return;
+  const bool is_k = row < p.Hkv, is_v = !is_k && row < 2 * p.Hkv, is_q = row >= 2 * p.Hkv;
+  const int h = is_q ? row - 2 * p.Hkv : is_v ? row - p.Hkv : row;
+  const RowLanes<D> lanes(p.r, li);
+  const int c0 = is_v ? 8 * li : lanes.c0, c1 = is_v ? 8 * li + 4 : lanes.c1;
+  if (is_v && p.v_pool == nullptr) return;       // boxes only: there are no values
+  const uint16_t* src = (is_k ? p.k + b * p.k_stride : is_v ? p.v + b * p.v_stride : p.q + b * p.q_stride) + h * D;
+  uint2 x = *reinterpret_cast<const uint2*>(src + c0), y = *reinterpret_cast<const uint2*>(src + c1);
+  const int sh = __builtin_ctz(p.S);
+  const int len = p.seq_lens[b] - p.lens_after;
+  if (len < 0) return;
+  const int j = len >> sh, slot = len & (p.S - 1);
+  const bool fits = j < p.Pmax;
+  const int phys = fits ? p.block_table[(size_t)b * p.Pmax + j] : -1;
+  if (!is_v) {
+    Angles ang;
+    load_angles(p.r, li, lanes.turns, [&](int axis) { return p.r.positions ? p.r.positions[(size_t)axis * p.r.T + b] : len; },
+                ang);
+    Norm n;
+    load_norm(is_q ? p.r.q_norm : p.r.k_norm, lanes.c0, lanes.c1, n);
+    rotate_row<D, kHalf>(p.r, lanes.turns, n, ang, x, y);
+  }
+  if (is_q) {
+    uint16_t* dst = p.q_out + b * p.q_out_stride + h * D;
+    *reinterpret_cast<uint2*>(dst + c0) = x;
+    *reinterpret_cast<uint2*>(dst + c1) = y;
+    return;
+  }
+  const bool store = p.v_pool != nullptr && phys >= 0 && phys < p.n_phys;
+  if (!fits || (p.v_pool != nullptr && !store)) return;
+  const StoredRow s = store_form<FMT, D>(x, y);
+  const PageTiles<FMT, D> tile(p, store ? phys : 0, h);
+  if (is_v) {
+    if constexpr (FMT == kPoolFp4) {
+      unsigned char* oct = tile.v + (slot >> 3) * (4 * D) + ((slot & 7) >> 1);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        unsigned char* dst = oct + 4 * Fp4Block<D>::word(8 * li + i);
+        const uint32_t code = (s.a.x >> (4 * i)) & 15u, was = *dst;
+        *dst = (unsigned char)((slot & 1) ? (was & 15u) | code << 4 : (was & 0xf0u) | code);
+      }
+    } else if constexpr (FMT == kPoolInt8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        tile.v[(size_t)(8 * li + i) * p.S + slot] = (uint8_t)((i < 4 ? s.a.x : s.b.x) >> (8 * (i & 3)));
+    } else {
+      const uint32_t w[4] = {s.a.x, s.a.y, s.b.x, s.b.y};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        reinterpret_cast<uint16_t*>(tile.v)[(size_t)(8 * li + i) * p.S + slot] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    }
+    if (li == 0) store_value_scale<FMT, D>(p, tile.k, tile.scale_row, slot, s.scale);
+    return;
+  }
+  if (p.v_pool != nullptr) store_key<FMT, D>(p, tile.k, tile.scale_row, slot, c0, c1, li, s);
+  float lo[8], hi[8];
+  stored_numbers<FMT>(s, lo, hi);
+  const size_t at = (((size_t)b * p.Hkv + h) * p.Pmax + j) * D;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int c = half ? c1 : c0;
+    uint2* lo_at = reinterpret_cast<uint2*>(p.page_min + at + c);
+    uint2* hi_at = reinterpret_cast<uint2*>(p.page_max + at + c);
+    if (slot != 0) {
+      const uint2 l = *lo_at, u = *hi_at;
+      const uint32_t lw[2] = {l.x, l.y}, uw[2] = {u.x, u.y};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lb = lw[i >> 1], ub = uw[i >> 1];
+        lo[4 * half + i] = fminf(lo[4 * half + i], i & 1 ? elem_hi<kHalf>(lb) : elem_lo<kHalf>(lb));
+        hi[4 * half + i] = fmaxf(hi[4 * half + i], i & 1 ? elem_hi<kHalf>(ub) : elem_lo<kHalf>(ub));
+      }
+    }
+    uint32_t l[4], u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      l[i] = box_number<FMT>(lo[4 * half + i], false);
+      u[i] = box_number<FMT>(hi[4 * half + i], true);
+    }
+    *lo_at = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
+    *hi_at = make_uint2(u[0] | u[1] << 16, u[2] | u[3] << 16);
+  }
+}
 
 // Which page of which sequence workgroup `task` has.  The sequences' touched pages are numbered through;
 // every wave works the same answer out.  False: there are fewer.
@@ -117,203 +346,191 @@ __device__ __forceinline__ bool find_page(const AppendParams& p, int sh, int tas
   return false;
 }
 
-// grid (touched pages or more, Hkv)
+// Minimum or maximum of a value over the lanes of the wave that hold the same channels.
+template <int LPR, bool kMax>
+__device__ __forceinline__ float over_groups(float v) {
+  auto take = [](float x, float y) { return kMax ? fmaxf(x, y) : fminf(x, y); };
+  if (LPR == 8)
+    v = take(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), kDppRowRor8, 0xf, 0xf, true)));
+  uint2s_t r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = take(__uint_as_float(r.x), __uint_as_float(r.y));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return take(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+
+// grid (touched pages or more, Hkv).  A token's key, value and queries are dealt to as many groups of
+// lanes as the workgroup has for each token, the rows asked for ahead of the lookups.  The extremes of the
+// keys as stored stay in the registers of the lanes that hold their channels, and meet over the wave's
+// groups and then, in LDS, over the waves.
 template <int FMT, int D>
 __global__ __launch_bounds__(kRotaryThreads) void append_rows_kernel(AppendParams p) {
   constexpr bool kHalf = FMT == kPoolFp16;
-  constexpr bool kQuant = FMT == kPoolInt8 || FMT == kPoolFp4;
   constexpr int LPR = D / 8, NG = kRotaryThreads / LPR;
   typedef AppendLds<FMT, D> Lds;
   typedef typename Lds::Elem Elem;
   extern __shared__ __align__(16) unsigned char smem[];
-  Elem* ks = reinterpret_cast<Elem*>(smem);
-  Elem* vs = ks + (size_t)p.S * Lds::kRow;
-  float* ksc = reinterpret_cast<float*>(vs + (size_t)p.S * Lds::kRow);   // scales of the slots
-  float* box = ksc + p.S;                                                // [2][parts][D]
+  Elem* vs = reinterpret_cast<Elem*>(smem);                                                  // [S][kRow]
+  float* box = reinterpret_cast<float*>(smem + (size_t)p.S * Lds::kRow * sizeof(Elem));      // [2][waves][D]
   const int sh = __builtin_ctz(p.S), h = blockIdx.y, tid = threadIdx.x;
-  int b, j, c0, n;
-  if (p.cu == nullptr) {
-    b = blockIdx.x;
-    c0 = b;
-    n = 1;
-    j = -1;
-  } else {
-    if (!find_page(p, sh, blockIdx.x, b, j)) return;
-    c0 = min(max(p.cu[b], 0), p.T);
-    n = min(max(p.cu[b + 1], 0), p.T) - c0;
-  }
-  n = uniform(n);
-  const int len = uniform(p.seq_lens[b] - (p.lens_after ? (p.cu ? p.cu[b + 1] - p.cu[b] : 1) : 0));
-  if (j < 0) j = len >> sh;
+  int b, j;
+  if (!find_page(p, sh, blockIdx.x, b, j)) return;
+  const int c0 = min(max(p.cu[b], 0), p.T), n = uniform(min(max(p.cu[b + 1], 0), p.T) - c0);
+  const int len = uniform(p.seq_lens[b] - (p.lens_after ? p.cu[b + 1] - p.cu[b] : 0));
   if (len < 0) return;                                   // (no such length)
   const int p0 = max(j << sh, len), p1 = min((j + 1) << sh, len + n);   // positions of this page's new tokens
   const int ntok = p1 - p0, slot0 = p0 - (j << sh), tok0 = c0 + p0 - len;
   const bool fits = (long long)len + n <= (long long)p.Pmax << sh;
   const int phys = uniform(fits ? p.block_table[(size_t)b * p.Pmax + j] : -1);
-  const bool store = fits && p.v_pool != nullptr && phys >= 0 && phys < p.n_phys;
-  const bool keep = store || (fits && p.v_pool == nullptr);     // the box follows the keys
-  unsigned char* ktile = p.k_pool + ((size_t)(store ? phys : 0) * p.Hkv + h) * (size_t)p.tile_stride;
-  unsigned char* vtile = FMT == kPoolFp4 ? ktile + Fp4Block<D>::values(p.S)
-                                         : p.v_pool + ((size_t)(store ? phys : 0) * p.Hkv + h) * (size_t)p.tile_stride;
-  const size_t scale_row = ((size_t)(store ? phys : 0) * p.Hkv + h) * (size_t)p.S;
-  // the rows of a token are dealt to as many of the workgroup's groups of lanes as there are for each token
+  const bool store = phys >= 0 && phys < p.n_phys;
+  const PageTiles<FMT, D> tile(p, store ? phys : 0, h);
   int tp = 1;
   while (tp < ntok && tp < NG) tp <<= 1;
-  const int group = tid / LPR, li = tid % LPR, first_row = group / tp, step = NG / tp;
+  const int group = tid / LPR, li = tid % LPR, part = group / tp, step = NG / tp;
   const RowLanes<D> lanes(p.r, li);
   Norm qn, kn;
   load_norm(p.r.q_norm, lanes.c0, lanes.c1, qn);
   load_norm(p.r.k_norm, lanes.c0, lanes.c1, kn);
-  // rows of a token: its key, its value, its query heads
-  const int rows = 2 + (p.q != nullptr ? p.G : 0);
-  for (int i0 = group % tp; i0 < ntok; i0 += tp) {   // (whole rows of lanes go round together)
+  const bool has_k = store && part == 0, has_v = store && part == (step > 1 ? 1 : 0);
+  const int G = p.q != nullptr ? p.G : 0;
+  const int g0 = step > 2 ? (part + step - 2) % step : part;          // queries go to the groups behind first
+  float lo[8], hi[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { lo[i] = INFINITY; hi[i] = -INFINITY; }
+  for (int i0 = group % tp; i0 < ntok; i0 += tp) {
     const int tok = tok0 + i0, slot = slot0 + i0;
+    constexpr int kAhead = 4;
+    const uint16_t* q_src = p.q + tok * p.q_stride + (size_t)h * p.G * D;
+    uint2 qa[kAhead], qb[kAhead], ka, kb, va, vb;
+    auto fetch = [&](int g) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (g + i * step < G) {
+          qa[i] = *reinterpret_cast<const uint2*>(q_src + (g + i * step) * D + lanes.c0);
+          qb[i] = *reinterpret_cast<const uint2*>(q_src + (g + i * step) * D + lanes.c1);
+        }
+    };
+    if (has_k) {
+      const uint16_t* src = p.k + tok * p.k_stride + h * D;
+      ka = *reinterpret_cast<const uint2*>(src + lanes.c0);
+      kb = *reinterpret_cast<const uint2*>(src + lanes.c1);
+    }
+    if (has_v) {
+      const uint16_t* src = p.v + tok * p.v_stride + h * D + 8 * li;
+      va = *reinterpret_cast<const uint2*>(src);
+      vb = *reinterpret_cast<const uint2*>(src + 4);
+    }
+    fetch(g0);
     Angles ang;
     load_angles(p.r, li, lanes.turns,
                 [&](int axis) { return p.r.positions ? p.r.positions[(size_t)axis * p.r.T + tok] : p0 + i0; }, ang);
-    for (int row = first_row; row < rows; row += step) {
-      if (row < 2 && !keep) continue;
-      if (row == 1 && !store) continue;
-      const uint16_t* src = row == 0   ? p.k + tok * p.k_stride + h * D
-                            : row == 1 ? p.v + tok * p.v_stride + h * D
-                                       : p.q + tok * p.q_stride + (h * p.G + row - 2) * D;
-      const int a0 = row == 1 ? 8 * li : lanes.c0, a1 = row == 1 ? 8 * li + 4 : lanes.c1;
-      uint2 x = *reinterpret_cast<const uint2*>(src + a0), y = *reinterpret_cast<const uint2*>(src + a1);
-      if (row >= 2) {
-        rotate_row<D, kHalf>(p.r, lanes.turns, qn, ang, x, y);
-        uint16_t* dst = p.q_out + tok * p.q_out_stride + (h * p.G + row - 2) * D;
-        *reinterpret_cast<uint2*>(dst + a0) = x;
-        *reinterpret_cast<uint2*>(dst + a1) = y;
-        continue;
-      }
-      if (row == 0) rotate_row<D, kHalf>(p.r, lanes.turns, kn, ang, x, y);
-      Elem* stage = (row == 0 ? ks : vs) + slot * Lds::kRow;
-      if constexpr (!kQuant) {
-        if (row == 0 && store) {
-          uint16_t* dst = reinterpret_cast<uint16_t*>(ktile) + slot * D;
-          *reinterpret_cast<uint2*>(dst + a0) = x;
-          *reinterpret_cast<uint2*>(dst + a1) = y;
-        }
-        *reinterpret_cast<uint2*>(stage + a0) = x;
-        *reinterpret_cast<uint2*>(stage + a1) = y;
-      } else {
-        const float f[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y),
-                            bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
-        float amax = 0.f;
+    if (has_k) {
+      rotate_row<D, kHalf>(p.r, lanes.turns, kn, ang, ka, kb);
+      const StoredRow s = store_form<FMT, D>(ka, kb);
+      store_key<FMT, D>(p, tile.k, tile.scale_row, slot, lanes.c0, lanes.c1, li, s);
+      float l[8], u[8];
+      stored_numbers<FMT>(s, l, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(f[i]));
-        amax = group_max_f32<LPR>(amax);
-        const float scale = FMT == kPoolInt8 ? i8_row_scale(amax) : fp4_row_scale(amax);
-        uint32_t c[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          c[i] = FMT == kPoolInt8 ? (uint32_t)i8_code(f[i], scale) & 0xffu : fp4_code(f[i], scale);
-        const uint32_t w0 = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, w1 = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
-        *reinterpret_cast<uint32_t*>(stage + a0) = w0;
-        *reinterpret_cast<uint32_t*>(stage + a1) = w1;
-        if (row == 0 && li == 0) ksc[slot] = scale;
-        if (store) {
-          if constexpr (FMT == kPoolInt8) {
-            if (row == 0) {
-              *reinterpret_cast<uint32_t*>(ktile + slot * D + a0) = w0;
-              *reinterpret_cast<uint32_t*>(ktile + slot * D + a1) = w1;
-            }
-            if (li == 0) (row == 0 ? p.k_scale : p.v_scale)[scale_row + slot] = scale;
-          } else {
-            if (row == 0) {
-              unsigned char* dst = ktile + slot * (D / 2);
-              *reinterpret_cast<uint16_t*>(dst + a0 / 2) = (uint16_t)(c[0] | c[1] << 4 | c[2] << 8 | c[3] << 12);
-              *reinterpret_cast<uint16_t*>(dst + a1 / 2) = (uint16_t)(c[4] | c[5] << 4 | c[6] << 8 | c[7] << 12);
-            }
-            if (li == 0) {
-              const int at = row == 0 ? Fp4Block<D>::key_scales(p.S) : Fp4Block<D>::value_scales(p.S);
-              *reinterpret_cast<uint16_t*>(ktile + at + 2 * slot) = (uint16_t)(__float_as_uint(scale) >> 16);
-            }
-          }
-        }
+      for (int i = 0; i < 8; ++i) {
+        lo[i] = fminf(lo[i], l[i]);
+        hi[i] = fmaxf(hi[i], u[i]);
       }
     }
+    if (has_v) {
+      const StoredRow s = store_form<FMT, D>(va, vb);
+      Elem* stage = vs + slot * Lds::kRow + 8 * li;
+      if constexpr (FMT == kPoolFp4) {
+        const uint32_t even = s.a.x & 0x0f0f0f0fu, odd = (s.a.x >> 4) & 0x0f0f0f0fu;     // a byte a code, in order
+        *reinterpret_cast<uint2*>(stage) = make_uint2(__builtin_amdgcn_perm(odd, even, 0x05010400u),
+                                                      __builtin_amdgcn_perm(odd, even, 0x07030602u));
+      } else if constexpr (FMT == kPoolInt8) {
+        *reinterpret_cast<uint2*>(stage) = make_uint2(s.a.x, s.b.x);
+      } else {
+        *reinterpret_cast<uint2*>(stage) = s.a;
+        *reinterpret_cast<uint2*>(stage + 4) = s.b;
+      }
+      if (li == 0) store_value_scale<FMT, D>(p, tile.k, tile.scale_row, slot, s.scale);
+    }
+    uint16_t* q_dst = p.q_out + tok * p.q_out_stride + (size_t)h * p.G * D;
+    for (int g = g0; g < G;) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (g + i * step < G) {
+          rotate_row<D, kHalf>(p.r, lanes.turns, qn, ang, qa[i], qb[i]);
+          *reinterpret_cast<uint2*>(q_dst + (g + i * step) * D + lanes.c0) = qa[i];
+          *reinterpret_cast<uint2*>(q_dst + (g + i * step) * D + lanes.c1) = qb[i];
+        }
+      g += kAhead * step;
+      fetch(g);
+    }
   }
-  if (!keep) return;
+  if (!store) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo[i] = over_groups<LPR, false>(lo[i]);
+    hi[i] = over_groups<LPR, true>(hi[i]);
+  }
+  if (lane_id() < LPR) {
+    float* mine = box + wave_id() * D;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      mine[lanes.c0 + i] = lo[i];
+      mine[lanes.c1 + i] = lo[4 + i];
+      mine[Lds::kWavesPer * D + lanes.c0 + i] = hi[i];
+      mine[Lds::kWavesPer * D + lanes.c1 + i] = hi[4 + i];
+    }
+  }
   __syncthreads();
   const int slot1 = slot0 + ntok;
-  // the box: a thread takes a channel, and every kParts-th token of it
-  const int c = tid % D, part = tid / D;
-  float lo = INFINITY, hi = -INFINITY;
-  for (int s = slot0 + part; s < slot1; s += Lds::kParts) {
-    const Elem e = ks[s * Lds::kRow + c];
-    float l, u;
-    if constexpr (FMT == kPoolInt8) {
-      const double x = (double)(int8_t)e * (double)ksc[s];
-      l = bf16_to_f32(bf16_directed(x, false));
-      u = bf16_to_f32(bf16_directed(x, true));
-    } else if constexpr (FMT == kPoolFp4) {
-      l = u = fp4_value(e) * ksc[s];
-    } else {
-      l = u = elem_to_f32<kHalf>(e);
-    }
-    lo = fminf(lo, l);
-    hi = fmaxf(hi, u);
-  }
-  box[part * D + c] = lo;
-  box[(Lds::kParts + part) * D + c] = hi;
-  // the values: channel-major, the tokens of a channel together
-  if (store) {
-    if constexpr (FMT == kPoolFp4) {
-      const int oct0 = slot0 >> 3, octs = ((slot1 + 7) >> 3) - oct0;
-      for (int i = tid; i < octs * D; i += kRotaryThreads) {
-        const int o = oct0 + i / D, w = i % D, ch = Fp4Block<D>::channel(w);
-        uint32_t word = 0u, mask = 0u;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const int s = 8 * o + t;
-          if (s >= slot0 && s < slot1) {
-            word |= (uint32_t)vs[s * Lds::kRow + ch] << (4 * t);
-            mask |= 15u << (4 * t);
-          }
-        }
-        uint32_t* dst = reinterpret_cast<uint32_t*>(vtile) + (size_t)o * D + w;
-        *dst = mask == 0xffffffffu ? word : (*dst & ~mask) | word;
-      }
-    } else {
-      constexpr int kMost = 16 / (int)sizeof(Elem);      // tokens in 16 bytes
-      const int chunk = min(kMost, p.S), csh = __builtin_ctz(chunk);
-      const int first = slot0 >> csh, chunks = ((slot1 + chunk - 1) >> csh) - first;
-      Elem* tile = reinterpret_cast<Elem*>(vtile);
-      for (int i = tid; i < chunks * D; i += kRotaryThreads) {
-        const int ch = i / chunks, s0 = (first + i % chunks) << csh;
-        Elem* dst = tile + (size_t)ch * p.S + s0;
-        if (s0 >= slot0 && s0 + chunk <= slot1 && chunk == kMost) {
-          uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-          for (int t = 0; t < kMost; ++t)
-            w[t * (int)sizeof(Elem) / 4] |= (uint32_t)vs[(s0 + t) * Lds::kRow + ch]
-                                            << (8 * sizeof(Elem) * (t % (4 / (int)sizeof(Elem))));
-          *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-          for (int t = max(s0, slot0); t < min(s0 + chunk, slot1); ++t) dst[t - s0] = vs[t * Lds::kRow + ch];
-        }
-      }
-    }
-  }
-  __syncthreads();
   if (tid < D) {
+    float l = box[tid], u = box[Lds::kWavesPer * D + tid];
 #pragma unroll
-    for (int i = 1; i < Lds::kParts; ++i) {
-      lo = fminf(lo, box[i * D + c]);
-      hi = fmaxf(hi, box[(Lds::kParts + i) * D + c]);
+    for (int i = 1; i < Lds::kWavesPer; ++i) {
+      l = fminf(l, box[i * D + tid]);
+      u = fmaxf(u, box[(Lds::kWavesPer + i) * D + tid]);
     }
-    const size_t at = (((size_t)b * p.Hkv + h) * p.Pmax + j) * D + c;
+    const size_t at = (((size_t)b * p.Hkv + h) * p.Pmax + j) * D + tid;
     if (slot0 != 0) {
-      lo = fminf(lo, elem_to_f32<kHalf>(p.page_min[at]));
-      hi = fmaxf(hi, elem_to_f32<kHalf>(p.page_max[at]));
+      l = fminf(l, elem_to_f32<kHalf>(p.page_min[at]));
+      u = fmaxf(u, elem_to_f32<kHalf>(p.page_max[at]));
     }
-    if constexpr (FMT == kPoolFp4) {
-      p.page_min[at] = (uint16_t)bf16_outwards(lo, false);
-      p.page_max[at] = (uint16_t)bf16_outwards(hi, true);
-    } else {
-      p.page_min[at] = kHalf ? f32_to_half(lo) : (uint16_t)(__float_as_uint(lo) >> 16);
-      p.page_max[at] = kHalf ? f32_to_half(hi) : (uint16_t)(__float_as_uint(hi) >> 16);
+    p.page_min[at] = box_number<FMT>(l, false);
+    p.page_max[at] = box_number<FMT>(u, true);
+  }
+  // the values: channel-major, the tokens of a channel together
+  if constexpr (FMT == kPoolFp4) {
+    const int oct0 = slot0 >> 3, octs = ((slot1 + 7) >> 3) - oct0;
+    for (int i = tid; i < octs * D; i += kRotaryThreads) {
+      const int o = oct0 + i / D, w = i % D, ch = Fp4Block<D>::channel(w);
+      uint32_t word = 0u, mask = 0u;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int s = 8 * o + t;
+        if (s >= slot0 && s < slot1) {
+          word |= (uint32_t)vs[s * Lds::kRow + ch] << (4 * t);
+          mask |= 15u << (4 * t);
+        }
+      }
+      uint32_t* dst = reinterpret_cast<uint32_t*>(tile.v) + (size_t)o * D + w;
+      *dst = mask == 0xffffffffu ? word : (*dst & ~mask) | word;
+    }
+  } else {
+    constexpr int kMost = 16 / (int)sizeof(Elem);      // tokens in 16 bytes
+    const int chunk = min(kMost, p.S), csh = __builtin_ctz(chunk);
+    const int first = slot0 >> csh, chunks = ((slot1 + chunk - 1) >> csh) - first;
+    Elem* dst_tile = reinterpret_cast<Elem*>(tile.v);
+    for (int i = tid; i < chunks * D; i += kRotaryThreads) {
+      const int ch = i / chunks, s0 = (first + i % chunks) << csh;
+      Elem* dst = dst_tile + (size_t)ch * p.S + s0;
+      if (s0 >= slot0 && s0 + chunk <= slot1 && chunk == kMost) {
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int t = 0; t < kMost; ++t)
+          w[t * (int)sizeof(Elem) / 4] |= (uint32_t)vs[(s0 + t) * Lds::kRow + ch]
+                                          << (8 * sizeof(Elem) * (t % (4 / (int)sizeof(Elem))));
+        *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+        for (int t = max(s0, slot0); t < min(s0 + chunk, slot1); ++t) dst[t - s0] = vs[t * Lds::kRow + ch];
+      }
     }
   }
 }

@@ -4,8 +4,9 @@
 // launch.  Fragments of 32 tokens: K (16 tokens x 32 channels a product) and V (16 channels x 32 tokens) are
 // expanded to bf16 in registers, one instruction for two codes, and go through v_mfma_f32_16x16x32_bf16;
 // the scales of 32 tokens multiply the logits (K) and the softmax weights (V) afterwards.  e2m1 numbers and
-// bf16 queries are exact operands; the weights go in as two bf16 numbers (nearest and the remainder's
-// nearest, 2^-18 relative), so nothing but the fp32 sums rounds.
+// bf16 queries are exact operands; the weights go in as three bf16 numbers (the nearest, the remainder's
+// nearest, and what is left: 2^-27 relative; with two an fp32 output was 2e-6 off, twice what the sums
+// cost), so nothing but the fp32 sums rounds.
 //   logits  St[token][head] = K[token][:] . Q^T[:][head]      row = token, column = head
 //   output  Ot[chan][head] += V^T[chan][token] . P^T[token][head]
 // Row 4 kb + i of logit tile t is token 8 kb + 4 t + i of the fragment (kb: quarter of the wave), so the eight
@@ -21,13 +22,19 @@
 
 namespace ts {
 
-constexpr int kFp4Waves = 4;
-constexpr int kFp4Threads = kFp4Waves * kWave;
-constexpr int kFp4Workgroups = 1024;    // most workgroups of a launch: four on each compute unit
 constexpr int kFp4Frag = 32;            // tokens of a fragment
 constexpr int kFp4List = 1024;          // list entries held in LDS at a time
-constexpr int kFp4MinShare = 4;         // fragments a workgroup has at the least
 constexpr int kFp4Parts = 64;           // about how many workgroups share a unit at the most
+
+// Workgroups of eight waves, two on each compute unit, for 64 channels; with 128 a wave needs more than the
+// 128 registers that leaves it (165), so four waves, three on each (1.1 GB of ragged sequences 276 -> 237 us).
+template <int D>
+struct Fp4Shape {
+  static constexpr int kWavesPer = D == 64 ? 8 : 4, kThreadsPer = kWavesPer * kWave;
+  static constexpr int kOccupancy = D == 64 ? 4 : 3;          // waves a SIMD
+  static constexpr int kResident = 256 * kOccupancy * 4 / kWavesPer;
+  static constexpr int kMinShare = 2 * kWavesPer;             // fragments a workgroup has at the least
+};
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -63,39 +70,61 @@ struct Fp4Frag {
   int valid;               // how many of the eight tokens exist
 };
 
-// One entry of the list: a physical page and how many tokens of it count.
-struct Fp4Entry {
-  int phys, tokens;
-};
+// One entry of the list: where a page's block of the unit's head begins, in units of 16 bytes, and in the low
+// eight bits how many of its tokens count.
+typedef uint64_t Fp4Entry;
+__device__ __forceinline__ Fp4Entry fp4_entry(const Fp4Params& p, int phys, int h, int tokens) {
+  return ((uint64_t)phys * p.Hkv + h) * (uint64_t)(p.tile_stride >> 4) << 8 | (uint64_t)tokens;
+}
 
-template <int D, int S>
-__device__ __forceinline__ void load_fp4(Fp4Frag<D>& f, const Fp4Params& p, const Fp4Entry* list, int frag, int h) {
+// Where fragment `frag` of the list keeps the eight tokens `oct`: the page's block and the first token's slot.
+template <int S>
+__device__ __forceinline__ const unsigned char* fp4_octet(const Fp4Params& p, const Fp4Entry* list, int frag, int oct,
+                                                          int& slot, int& tokens) {
   constexpr int PPF = S < kFp4Frag ? kFp4Frag / S : 1, FPP = S > kFp4Frag ? S / kFp4Frag : 1;
-  typedef Fp4Block<D> Block;
-  const int lane = lane_id(), r = lane & 15, kb = lane >> 4, ko = r >> 2;   // octets of the key rows, of the rest
-  const int first = frag / FPP * PPF, half = FPP > 1 ? kFp4Frag * (frag % FPP) : 0;
-  const Fp4Entry ek = list[first + (PPF > 1 ? 8 * ko / S : 0)], ev = list[first + (PPF > 1 ? 8 * kb / S : 0)];
-  const int kslot = half + (8 * ko) % (S < kFp4Frag ? S : kFp4Frag) + (r & 3);
-  const int slot = half + (8 * kb) % (S < kFp4Frag ? S : kFp4Frag);
-  const unsigned char* kt = p.pool + ((size_t)ek.phys * p.Hkv + h) * (size_t)p.tile_stride;
-  const unsigned char* vt = p.pool + ((size_t)ev.phys * p.Hkv + h) * (size_t)p.tile_stride;
+  const Fp4Entry e = list[frag / FPP * PPF + (PPF > 1 ? 8 * oct / S : 0)];
+  slot = (FPP > 1 ? kFp4Frag * (frag % FPP) : 0) + (8 * oct) % (S < kFp4Frag ? S : kFp4Frag);
+  uint32_t lo = (uint32_t)e, hi = (uint32_t)(e >> 32);
+  if (PPF == 1) {      // the same page for all lanes
+    lo = (uint32_t)uniform((int)lo);
+    hi = (uint32_t)uniform((int)hi);
+  }
+  tokens = (int)(lo & 0xffu);
+  return p.pool + ((((uint64_t)hi << 32 | (lo & ~0xffu)) >> 4));
+}
+
+// The keys: rows of tokens 8 (r / 4) + r % 4 and 4 on, r = lane % 16; the scales of this quarter's tokens.
+template <int D, int S>
+__device__ __forceinline__ void load_fp4_keys(Fp4Frag<D>& f, const Fp4Params& p, const Fp4Entry* list, int frag) {
+  const int lane = lane_id(), r = lane & 15, kb = lane >> 4;
+  int slot, tokens;
+  const unsigned char* row = fp4_octet<S>(p, list, frag, r >> 2, slot, tokens);
+  row += (slot + (r & 3)) * (D / 2) + kb * (D / 8);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const unsigned char* row = kt + (kslot + 4 * t) * (D / 2) + kb * (D / 8);
     if constexpr (D == 128) {
-      const uint4 w = *reinterpret_cast<const uint4*>(row);
+      const uint4 w = *reinterpret_cast<const uint4*>(row + 4 * t * (D / 2));
       f.k[t][0] = w.x; f.k[t][1] = w.y; f.k[t][2] = w.z; f.k[t][3] = w.w;
     } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(row);
+      const uint2 w = *reinterpret_cast<const uint2*>(row + 4 * t * (D / 2));
       f.k[t][0] = w.x; f.k[t][1] = w.y;
     }
   }
-  const unsigned char* vrow = vt + Block::values(S) + (slot / 8) * (4 * D) + r * 16;
+  const unsigned char* tile = fp4_octet<S>(p, list, frag, kb, slot, tokens);
+  f.ks = *reinterpret_cast<const uint4*>(tile + Fp4Block<D>::key_scales(S) + 2 * slot);
+  f.valid = tokens - slot;
+}
+
+// The values of this quarter's tokens and their scales.
+template <int D, int S>
+__device__ __forceinline__ void load_fp4_values(Fp4Frag<D>& f, const Fp4Params& p, const Fp4Entry* list, int frag) {
+  const int lane = lane_id(), r = lane & 15, kb = lane >> 4;
+  int slot, tokens;
+  const unsigned char* tile = fp4_octet<S>(p, list, frag, kb, slot, tokens);
+  const unsigned char* row = tile + Fp4Block<D>::values(S) + (slot / 8) * (4 * D) + r * 16;
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) f.v[i] = *reinterpret_cast<const uint4*>(vrow + 256 * i);
-  f.ks = *reinterpret_cast<const uint4*>(vt + Block::key_scales(S) + 2 * slot);
-  f.vs = *reinterpret_cast<const uint4*>(vt + Block::value_scales(S) + 2 * slot);
-  f.valid = ev.tokens - slot;
+  for (int i = 0; i < D / 64; ++i) f.v[i] = *reinterpret_cast<const uint4*>(row + 256 * i);
+  f.vs = *reinterpret_cast<const uint4*>(tile + Fp4Block<D>::value_scales(S) + 2 * slot);
 }
 
 // Running softmax state of a wave: per lane the head lane % 16.
@@ -105,24 +134,35 @@ struct Fp4State {
   float m, l;             // running maximum (log2 units, the same in the four quarters), this quarter's sum
 };
 
-template <int D>
-__device__ __forceinline__ void attend_fp4(Fp4State<D>& st, const Fp4Frag<D>& f, const bf16x8_t (&q)[D / 32], float scale_log2) {
-  float s[8], ks[8], vs[8];
-  unpack8(f.ks, ks);
-  unpack8(f.vs, vs);
+// One fragment; with kMore the one behind it (next) is fetched piece by piece into the registers that this
+// one leaves: its keys go out behind the first product, its values behind the second.
+template <int D, int S, bool kMore>
+__device__ __forceinline__ void attend_fp4(Fp4State<D>& st, Fp4Frag<D>& f, const bf16x8_t (&q)[D / 32], const Fp4Params& p,
+                                           const Fp4Entry* list, int next) {
+  float s[8];
+  {
+    float ks[8];
+    unpack8(f.ks, ks);
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    float4_t c = {0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 2; ++t) {
+      float4_t c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_operand(f.k[t][i]), q[i], c, 0, 0, 0);
+      for (int i = 0; i < D / 32; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_operand(f.k[t][i]), q[i], c, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[4 * t + i] = c[i] * (ks[4 * t + i] * scale_log2);
+      for (int i = 0; i < 4; ++i) s[4 * t + i] = c[i] * (ks[4 * t + i] * p.scale_log2);
+    }
   }
-  if (__any(f.valid < 8)) {   // slots without a token may hold anything, scales included
+  const int valid = f.valid;
+  __builtin_amdgcn_sched_barrier(0);
+  if (kMore) load_fp4_keys<D, S>(f, p, list, next);
+  __builtin_amdgcn_sched_barrier(0);
+  float vs[8];
+  unpack8(f.vs, vs);
+  if (__any(valid < 8)) {   // slots without a token may hold anything, scales included
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      s[i] = i < f.valid ? s[i] : -INFINITY;
-      vs[i] = i < f.valid ? vs[i] : 0.f;
+      s[i] = i < valid ? s[i] : -INFINITY;
+      vs[i] = i < valid ? vs[i] : 0.f;
     }
   }
   float m = s[0];
@@ -137,23 +177,31 @@ __device__ __forceinline__ void attend_fp4(Fp4State<D>& st, const Fp4Frag<D>& f,
     for (int cb = 0; cb < D / 16; ++cb) st.acc[cb] *= a;
     st.m = m;
   }
-  bf16x8_t hi, lo;
+  bf16x8_t hi, lo, rest;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float w = __builtin_amdgcn_exp2f(s[i] - ref);
     st.l += w;
     const float x = w * vs[i];
     hi[i] = (__bf16)x;
-    lo[i] = (__bf16)(x - (float)hi[i]);
+    const float y = x - (float)hi[i];
+    lo[i] = (__bf16)y;
+    rest[i] = (__bf16)(y - (float)lo[i]);
   }
+  auto word = [&](int cb) {
+    const uint4 w = f.v[cb / 4];
+    return cb % 4 == 0 ? w.x : cb % 4 == 1 ? w.y : cb % 4 == 2 ? w.z : w.w;
+  };
 #pragma unroll
   for (int cb = 0; cb < D / 16; ++cb) {
-    const uint4 w4 = f.v[cb / 4];
-    const uint32_t w = cb % 4 == 0 ? w4.x : cb % 4 == 1 ? w4.y : cb % 4 == 2 ? w4.z : w4.w;
-    const bf16x8_t v = fp4_operand(w);
-    st.acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, st.acc[cb], 0, 0, 0);
+    const bf16x8_t v = fp4_operand(word(cb));
+    st.acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, rest, st.acc[cb], 0, 0, 0);
     st.acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, st.acc[cb], 0, 0, 0);
+    st.acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, st.acc[cb], 0, 0, 0);
   }
+  __builtin_amdgcn_sched_barrier(0);
+  if (kMore) load_fp4_values<D, S>(f, p, list, next);
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int S, bool kSparse>
@@ -172,7 +220,8 @@ __device__ __forceinline__ void store_fp4_out(const Fp4Params& p, size_t idx, fl
 }
 
 template <int D, int S, bool kSparse>
-__global__ __launch_bounds__(kFp4Threads) void fp4_attention_kernel(Fp4Params p) {
+__global__ __launch_bounds__(Fp4Shape<D>::kThreadsPer, Fp4Shape<D>::kOccupancy) void fp4_attention_kernel(Fp4Params p) {
+  constexpr int kFp4Waves = Fp4Shape<D>::kWavesPer, kFp4Threads = Fp4Shape<D>::kThreadsPer;
   constexpr int PPF = S < kFp4Frag ? kFp4Frag / S : 1, FPP = S > kFp4Frag ? S / kFp4Frag : 1;
   constexpr int kFrags = (kFp4List + 1 - FPP) * FPP / PPF;   // fragments the list in LDS covers, begun within a page too
   constexpr int kRow = D + 4;                        // a head's merged row: channels, maximum, sum
@@ -184,10 +233,12 @@ __global__ __launch_bounds__(kFp4Threads) void fp4_attention_kernel(Fp4Params p)
 
   // all fragments of the launch, and where this workgroup's begin
   uint32_t total = 0;
-  int longest = 0;
+  int longest = 0, mine = 0, upto = 0;     // of a wave's last 64 sequences: this lane's fragments, up to here
   for (int base = 0; base < p.B; base += kWave) {
     const int i = base + lane, f = i < p.B ? fp4_frags<S, kSparse>(p, i) : 0;
-    total += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_sum(f), kWave - 1);
+    mine = f;
+    upto = wave_inclusive_sum(f);
+    total += (uint32_t)__builtin_amdgcn_readlane(upto, kWave - 1);
     longest = max(longest, (int)wave_max_u32((uint32_t)f));
     // a sequence without tokens has zeros
     if (blockIdx.x == 0 && wave == 0) {
@@ -202,7 +253,7 @@ __global__ __launch_bounds__(kFp4Threads) void fp4_attention_kernel(Fp4Params p)
     }
   }
   total *= (uint32_t)p.Hkv;
-  const uint32_t share = max(max((uint32_t)kFp4MinShare, (total + gridDim.x - 1) / gridDim.x),
+  const uint32_t share = max(max((uint32_t)Fp4Shape<D>::kMinShare, (total + gridDim.x - 1) / gridDim.x),
                              (uint32_t)((longest + kFp4Parts - 1) / kFp4Parts));
   uint32_t at = blockIdx.x * share;
   const uint32_t end = min(total, at + share);
@@ -210,14 +261,16 @@ __global__ __launch_bounds__(kFp4Threads) void fp4_attention_kernel(Fp4Params p)
   int b = 0, nf = 0;
   uint32_t ustart = 0;    // first fragment of the unit
   for (int base = 0, before = 0; base < p.B; base += kWave) {
-    const int i = base + lane, f = i < p.B ? fp4_frags<S, kSparse>(p, i) : 0;
-    const int upto = before + wave_inclusive_sum(f);
-    const uint32_t first = (uint32_t)(upto - f) * p.Hkv;
-    const uint64_t mine = __ballot(at >= first && at < (uint32_t)upto * p.Hkv);
-    if (mine != 0) {
-      const int src = __builtin_ctzll(mine);
+    if (p.B > kWave) {      // (up to 64 sequences the lanes have them still)
+      mine = base + lane < p.B ? fp4_frags<S, kSparse>(p, base + lane) : 0;
+      upto = before + wave_inclusive_sum(mine);
+    }
+    const uint32_t first = (uint32_t)(upto - mine) * p.Hkv;
+    const uint64_t here = __ballot(at >= first && at < (uint32_t)upto * p.Hkv);
+    if (here != 0) {
+      const int src = __builtin_ctzll(here);
       b = uniform(base + src);
-      nf = __builtin_amdgcn_readlane(f, src);
+      nf = __builtin_amdgcn_readlane(mine, src);
       ustart = (uint32_t)__builtin_amdgcn_readlane((int)first, src);
       break;
     }
@@ -256,14 +309,17 @@ __global__ __launch_bounds__(kFp4Threads) void fp4_attention_kernel(Fp4Params p)
         on = on && page >= 0 && page < p.Pmax;
         const int phys = p.block_table[(size_t)b * p.Pmax + (on ? page : 0)];
         on = on && phys >= 0 && phys < p.n_phys;
-        list[i].phys = on ? phys : 0;
-        list[i].tokens = on ? min(max(len - page * S, 0), S) : 0;
+        list[i] = on ? fp4_entry(p, phys, h, min(max(len - page * S, 0), S)) : fp4_entry(p, 0, h, 0);
       }
       __syncthreads();
-      for (int f = c0 + wave; f < c1; f += kFp4Waves) {
+      const int shift = c0 % FPP - c0;      // fragments as the list has them
+      if (c0 + wave < c1) {
         Fp4Frag<D> fr;
-        load_fp4<D, S>(fr, p, list, f - c0 + c0 % FPP, h);
-        attend_fp4<D>(st, fr, q, p.scale_log2);
+        int f = c0 + wave + shift;
+        load_fp4_keys<D, S>(fr, p, list, f);
+        load_fp4_values<D, S>(fr, p, list, f);
+        for (; f + kFp4Waves < c1 + shift; f += kFp4Waves) attend_fp4<D, S, true>(st, fr, q, p, list, f + kFp4Waves);
+        attend_fp4<D, S, false>(st, fr, q, p, list, 0);
       }
     }
     // the waves' results: head rows of channels, maximum, sum
@@ -319,33 +375,42 @@ __global__ __launch_bounds__(kFp4Threads) void fp4_attention_kernel(Fp4Params p)
       }
       __syncthreads();
       if (uniform(last_one)) {
+        // maxima and sums of all parts into LDS, their weights over the common maximum from there
+        const int parts = (int)(w1 - w0) + 1;
+        auto part_of = [&](int e) {
+          const uint32_t w = w0 + (uint32_t)e;
+          return p.part + ((size_t)w * 2 + (w * share > ustart ? 0 : 1)) * p.G * (D + 2);
+        };
+        float* tops = merge;                        // [parts][G]
+        float* sums = merge + parts * p.G;          // [parts][G]
+        constexpr int kAhead = 8;                   // parts asked for together
+        float x[kAhead];
+        auto fetch = [&](int i, int e0) {
+#pragma unroll
+          for (int e = 0; e < kAhead; ++e) x[e] = load_agent(part_of(min(e0 + e, parts - 1)) + i / D * (D + 2) + i % D);
+        };
+        if (tid < p.G * D) fetch(tid, 0);
+        for (int i = tid; i < parts * p.G; i += kFp4Threads) {
+          const float* row = part_of(i / p.G) + (i % p.G) * (D + 2) + D;
+          tops[i] = load_agent(row);
+          sums[i] = load_agent(row + 1);
+        }
+        __syncthreads();
         for (int i = tid; i < p.G * D; i += kFp4Threads) {
           const int g = i / D, c = i % D;
           float M = -INFINITY, o = 0.f, sum = 0.f;
-          constexpr int kAhead = 8;      // parts asked for together
-          for (uint32_t w = w0; w <= w1; w += kAhead) {
-            float m[kAhead], x[kAhead], z[kAhead];
+          for (int e = 0; e < parts; ++e) M = fmaxf(M, tops[e * p.G + g]);
+          const float ref = M == -INFINITY ? 0.f : M;
+          for (int e0 = 0; e0 < parts; e0 += kAhead) {
+            if (e0 != 0 || i != tid) fetch(i, e0);
 #pragma unroll
             for (int e = 0; e < kAhead; ++e) {
-              const uint32_t v = min(w + e, w1);
-              const float* part = p.part + ((size_t)v * 2 + (v * share > ustart ? 0 : 1)) * p.G * (D + 2) + g * (D + 2);
-              m[e] = load_agent(part + D);
-              x[e] = load_agent(part + c);
-              z[e] = load_agent(part + D + 1);
+              if (e0 + e < parts) {
+                const float a = __builtin_amdgcn_exp2f(tops[(e0 + e) * p.G + g] - ref);
+                o += x[e] * a;
+                sum += sums[(e0 + e) * p.G + g] * a;
+              }
             }
-            float top = M;
-#pragma unroll
-            for (int e = 0; e < kAhead; ++e) top = fmaxf(top, m[e]);
-            const float ref = top == -INFINITY ? 0.f : top, a = __builtin_amdgcn_exp2f(M - ref);
-            o *= a;
-            sum *= a;
-#pragma unroll
-            for (int e = 0; e < kAhead; ++e) {
-              const float k = w + e <= w1 ? __builtin_amdgcn_exp2f(m[e] - ref) : 0.f;
-              o += x[e] * k;
-              sum += z[e] * k;
-            }
-            M = top;
           }
           const size_t head = (size_t)b * p.Hq + h * p.G + g;
           store_fp4_out(p, head * D + c, sum > 0.f ? o / sum : 0.f);

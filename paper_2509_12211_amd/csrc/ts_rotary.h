@@ -107,10 +107,19 @@ __device__ __forceinline__ void load_norm(const float* w, int c0, int c1, Norm& 
   n.w[4] = b.x; n.w[5] = b.y; n.w[6] = b.z; n.w[7] = b.w;
 }
 
+// Two fp32 numbers as 16-bit ones, to nearest even.
 template <bool kHalf>
 __device__ __forceinline__ uint32_t pack_elems(float x, float y) {
   if (kHalf) return (uint32_t)f32_to_half(x) | (uint32_t)f32_to_half(y) << 16;
-  return (uint32_t)f32_to_bf16_rn(x) | (uint32_t)f32_to_bf16_rn(y) << 16;
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+}
+
+// 1 / sqrt(m): the instruction's estimate y (good to 2^-22 or better), and with e = 1 - m y^2 the series
+// y (1 + e / 2 + 3 e^2 / 8), which leaves the last bits of fp64.
+__device__ __forceinline__ double inverse_root(double m) {
+  const double y = __builtin_amdgcn_rsq(m), e = fma(-m * y, y, 1.0);
+  return fma(y * e, fma(0.375, e, 0.5), y);
 }
 
 // One row, eight channels a lane: normed, rotated and rounded to 16 bits.  All lanes of the row take part.
@@ -125,7 +134,7 @@ __device__ __forceinline__ void rotate_row(const RotaryParams& p, bool turns, co
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum = fma((double)y[i], (double)y[i], sum);
     sum = group_sum1_f64<D / 8>(sum);
-    const float r = (float)(1.0 / sqrt(sum * (1.0 / D) + (double)p.eps));
+    const float r = (float)inverse_root(sum * (1.0 / D) + (double)p.eps);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = (y[i] * r) * n.w[i];
   }
@@ -163,32 +172,55 @@ struct RotateParams {
 };
 
 // grid (tokens / tokens_per_wg, heads / rows_per_wg).  A row's lanes stay with their token, whose angles
-// they hold, and take its heads in turn.  Memory-bound: every element is read and written once.
+// they hold, and take its heads in turn, kRowsAhead rows on their way at a time.  Memory-bound: every
+// element is read and written once.
+constexpr int kRowsAhead = 4;
 template <int D, bool kHalf>
 __global__ __launch_bounds__(kRotaryThreads) void rotate_rows_kernel(RotateParams p) {
   constexpr int LPR = D / 8, NG = kRotaryThreads / LPR;
   const int group = threadIdx.x / LPR, li = threadIdx.x % LPR;
   const int t = blockIdx.x * p.tokens_per_wg + group % p.tokens_per_wg, step = NG / p.tokens_per_wg;
-  const bool on = t < p.T;
-  const int tc = on ? t : p.T - 1;
+  if (t >= p.T) return;      // (whole groups of lanes; there is no barrier)
   const RowLanes<D> lanes(p.r, li);
+  const int rows = p.Hq + p.Hkv, end = min(rows, (int)(blockIdx.y + 1) * p.rows_per_wg);
+  const int first = blockIdx.y * p.rows_per_wg + group / p.tokens_per_wg;
+  const uint16_t *q = p.q + t * p.q_stride, *k = p.k + t * p.k_stride - p.Hq * D;
+  uint16_t *q_out = p.q_out + t * p.q_out_stride, *k_out = p.k_out + t * p.k_out_stride - p.Hq * D;
+  uint2 a[kRowsAhead], b[kRowsAhead];
+  auto fetch = [&](int row0) {
+#pragma unroll
+    for (int i = 0; i < kRowsAhead; ++i) {
+      const int row = row0 + i * step;
+      if (row < end) {
+        const uint16_t* src = (row < p.Hq ? q : k) + row * D;
+        a[i] = *reinterpret_cast<const uint2*>(src + lanes.c0);
+        b[i] = *reinterpret_cast<const uint2*>(src + lanes.c1);
+      }
+    }
+  };
+  fetch(first);
   Angles ang;
-  load_angles(p.r, li, lanes.turns, [&](int axis) { return p.r.positions[(size_t)axis * p.r.T + tc]; }, ang);
+  load_angles(p.r, li, lanes.turns, [&](int axis) { return p.r.positions[(size_t)axis * p.r.T + t]; }, ang);
   Norm qn, kn;
   load_norm(p.r.q_norm, lanes.c0, lanes.c1, qn);
   load_norm(p.r.k_norm, lanes.c0, lanes.c1, kn);
-  const int rows = p.Hq + p.Hkv, end = min(rows, (int)(blockIdx.y + 1) * p.rows_per_wg);
-  for (int row = blockIdx.y * p.rows_per_wg + group / p.tokens_per_wg; row < end; row += step) {
-    const bool is_q = row < p.Hq;
-    const uint16_t* src = is_q ? p.q + tc * p.q_stride + row * D : p.k + tc * p.k_stride + (row - p.Hq) * D;
-    uint16_t* dst = is_q ? p.q_out + tc * p.q_out_stride + row * D : p.k_out + tc * p.k_out_stride + (row - p.Hq) * D;
-    uint2 a = *reinterpret_cast<const uint2*>(src + lanes.c0), b = *reinterpret_cast<const uint2*>(src + lanes.c1);
-    if (is_q) rotate_row<D, kHalf>(p.r, lanes.turns, qn, ang, a, b);
-    else rotate_row<D, kHalf>(p.r, lanes.turns, kn, ang, a, b);
-    if (on) {
-      *reinterpret_cast<uint2*>(dst + lanes.c0) = a;
-      *reinterpret_cast<uint2*>(dst + lanes.c1) = b;
+  for (int row0 = first; row0 < end;) {
+#pragma unroll
+    for (int i = 0; i < kRowsAhead; ++i) {
+      const int row = row0 + i * step;
+      if (row < end) {
+        Norm n;
+        n.on = row < p.Hq ? qn.on : kn.on;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) n.w[c] = row < p.Hq ? qn.w[c] : kn.w[c];
+        rotate_row<D, kHalf>(p.r, lanes.turns, n, ang, a[i], b[i]);
+        uint16_t* dst = (row < p.Hq ? q_out : k_out) + row * D;
+        *reinterpret_cast<uint2*>(dst + lanes.c0) = a[i];
+        *reinterpret_cast<uint2*>(dst + lanes.c1) = b[i];
+      }
     }
+    row0 += kRowsAhead * step;
+    fetch(row0);
   }
 }
 

@@ -305,6 +305,35 @@ def test_sequences_that_do_not_fit_and_bad_pages(fmt):
         assert torch.equal(gv, stored(v[a:a + m].cpu(), fmt).transpose(0, 1))
 
 
+@pytest.mark.parametrize("one_each", [False, True])
+def test_four_bit_numbers_at_their_borders(one_each):
+    """Rows whose numbers lie on the borders between codes, just beside them, and on either side of zero, at
+    scales from the smallest to the largest; a row of infinities and NaN."""
+    d, S, wide = 64, 8, 9
+    border = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    rows = []
+    for scale in (1.0, 1.5, 2.0 ** -100, 3 * 2.0 ** -120, 1.25 * 2.0 ** 90, 2.0 ** 125, 2.0 ** -133):
+        x = torch.cat([border, -border, torch.tensor([6.0, -6.0, 0.0, -0.0])]).double() * scale
+        up, down = (x.to(BF).view(torch.int16) + 1).view(BF), (x.to(BF).view(torch.int16) - 1).view(BF)
+        row = torch.cat([x.to(BF), up[:14], down[:14], torch.zeros(18).to(BF)])
+        rows.append(torch.where(row.abs().double() <= 6 * scale, row, torch.zeros_like(row)))
+    k = torch.stack(rows)[:, None].contiguous()
+    B, n = (k.shape[0], 1) if one_each else (1, k.shape[0])
+    v = (k * 1).flip(-1).contiguous()
+    c = Cache("fp4", B, 1, d, S, wide, torch.Generator().manual_seed(1))
+    cu = None if one_each else torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    ts.append_rows(c.layout, k.to(DEV), v.to(DEV), cu_tokens=cu)
+    held = [[k[b:b + 1], v[b:b + 1]] for b in range(B)] if one_each else [[k, v]]
+    assert_cache(c, held, "borders")
+    # not finite: the largest number of the row's scale, and zero
+    x = torch.zeros((B if one_each else 1, 1, d), dtype=BF)
+    x[..., 0], x[..., 1], x[..., 2], x[..., 3] = math.inf, -math.inf, math.nan, 1.0
+    c.lens.zero_()
+    ts.append_rows(c.layout, x.to(DEV), x.to(DEV), cu_tokens=None if one_each else torch.tensor([0, 1], dtype=torch.int32, device=DEV))
+    for held in c.held(0, 1):
+        assert torch.isfinite(held).all() and held[0, 0, 0] == -held[0, 0, 1] > 3e38 and (held[0, 0, 2:] == 0).all()
+
+
 def test_many_sequences_of_few_tokens():
     """More sequences than a wave has lanes, most of them without a new token."""
     g = torch.Generator().manual_seed(9)
