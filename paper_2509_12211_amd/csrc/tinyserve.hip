@@ -431,18 +431,28 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
   p.out_bf16 = L->out_format == TS_OUT_BF16;
   p.tile_stride = tile_stride_of(L);
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
-  const int waves = L->head_dim == 64 ? Fp4Shape<64>::kWavesPer : Fp4Shape<128>::kWavesPer;
-  const size_t lds = kFp4List * sizeof(Fp4Entry) + (size_t)waves * p.G * (L->head_dim + 4) * sizeof(float);
   int st = TS_OK;
-#define TS_LAUNCH_FP4(DD, SS, SPARSE)                                              \
+#define TS_LAUNCH_FP4(DD, SS, SPARSE, NARROW, OUT)                                 \
   do {                                                                             \
-    if ((st = allow_lds(fp4_attention_kernel<DD, SS, SPARSE>, lds)) != TS_OK) return st; \
-    fp4_attention_kernel<DD, SS, SPARSE><<<pl.workgroups, waves * kWave, lds, stream>>>(p); \
+    constexpr size_t lds = Fp4Shape<DD>::lds();                                    \
+    const auto kernel = fp4_attention_kernel<DD, SS, SPARSE, NARROW, OUT>;         \
+    if ((st = allow_lds(kernel, lds)) != TS_OK) return st;                         \
+    kernel<<<pl.workgroups, Fp4Shape<DD>::kThreadsPer, lds, stream>>>(p);          \
+  } while (0)
+#define TS_LAUNCH_FP4_OUT(DD, SS, SPARSE, NARROW)                \
+  do {                                                           \
+    if (p.out_bf16) TS_LAUNCH_FP4(DD, SS, SPARSE, NARROW, false); \
+    else TS_LAUNCH_FP4(DD, SS, SPARSE, NARROW, true);            \
+  } while (0)
+#define TS_LAUNCH_FP4_HEADS(DD, SS, SPARSE)                      \
+  do {                                                           \
+    if (p.G <= 8) TS_LAUNCH_FP4_OUT(DD, SS, SPARSE, true);       \
+    else TS_LAUNCH_FP4_OUT(DD, SS, SPARSE, false);               \
   } while (0)
 #define TS_LAUNCH_FP4_LIST(DD, SS)                      \
   do {                                                  \
-    if (sel) TS_LAUNCH_FP4(DD, SS, true);               \
-    else TS_LAUNCH_FP4(DD, SS, false);                  \
+    if (sel) TS_LAUNCH_FP4_HEADS(DD, SS, true);         \
+    else TS_LAUNCH_FP4_HEADS(DD, SS, false);            \
   } while (0)
 #define TS_LAUNCH_FP4_PAGE(DD)                                  \
   do {                                                          \
@@ -455,6 +465,8 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
   else TS_LAUNCH_FP4_PAGE(128);
 #undef TS_LAUNCH_FP4_PAGE
 #undef TS_LAUNCH_FP4_LIST
+#undef TS_LAUNCH_FP4_HEADS
+#undef TS_LAUNCH_FP4_OUT
 #undef TS_LAUNCH_FP4
   return launch_status();
 }

@@ -363,7 +363,7 @@ __device__ __forceinline__ float over_groups(float v) {
 // keys as stored stay in the registers of the lanes that hold their channels, and meet over the wave's
 // groups and then, in LDS, over the waves.
 template <int FMT, int D>
-__global__ __launch_bounds__(kRotaryThreads) void append_rows_kernel(AppendParams p) {
+__global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendParams p) {
   constexpr bool kHalf = FMT == kPoolFp16;
   constexpr int LPR = D / 8, NG = kRotaryThreads / LPR;
   typedef AppendLds<FMT, D> Lds;

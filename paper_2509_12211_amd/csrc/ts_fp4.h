@@ -26,14 +26,21 @@ constexpr int kFp4Frag = 32;            // tokens of a fragment
 constexpr int kFp4List = 1024;          // list entries held in LDS at a time
 constexpr int kFp4Parts = 64;           // about how many workgroups share a unit at the most
 
-// Workgroups of eight waves, two on each compute unit, for 64 channels; with 128 a wave needs more than the
-// 128 registers that leaves it (165), so four waves, three on each (1.1 GB of ragged sequences 276 -> 237 us).
+// Workgroups of eight waves, two on a compute unit, for 64 channels; with 128, where a wave's registers leave
+// room for three on a SIMD and no less, of four, three on a unit (ragged batch of 1.1 GB 232 -> 223 us, lists of
+// a quarter of the pages 23.2 -> 20.5; with 64 channels the smaller ones lose, 24.3 -> 28.8 and 11.9 -> 15.6).
 template <int D>
 struct Fp4Shape {
   static constexpr int kWavesPer = D == 64 ? 8 : 4, kThreadsPer = kWavesPer * kWave;
-  static constexpr int kOccupancy = D == 64 ? 4 : 3;          // waves a SIMD
-  static constexpr int kResident = 256 * kOccupancy * 4 / kWavesPer;
+  static constexpr int kPerCu = D == 64 ? 2 : 3;              // workgroups on a compute unit
+  static constexpr int kStages = D == 64 ? 3 : 2;             // fragments a wave has room for
+  static constexpr int kResident = 256 * kPerCu;
   static constexpr int kMinShare = 2 * kWavesPer;             // fragments a workgroup has at the least
+  // a fragment in LDS: keys, values, scales
+  static constexpr int kKeys = 0, kValues = 16 * D, kScales = 32 * D, kStage = 32 * D + 256;
+  static constexpr int kLoads = D / 32 + 1;                   // loads that bring it
+  static constexpr int kRing = kStages * kStage;              // bytes of a wave
+  static constexpr size_t lds() { return (size_t)kFp4List * 8 + (size_t)kWavesPer * kRing; }
 };
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -62,112 +69,190 @@ __device__ __forceinline__ bf16x8_t fp4_operand(uint32_t w) {
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-template <int D>
-struct Fp4Frag {
-  uint32_t k[2][D / 32];   // this lane's D / 4 channels of its two tokens
-  uint4 v[D / 64];         // this lane's eight tokens of D / 16 channels
-  uint4 ks, vs;            // the eight tokens' scales
-  int valid;               // how many of the eight tokens exist
-};
-
-// One entry of the list: where a page's block of the unit's head begins, in units of 16 bytes, and in the low
-// eight bits how many of its tokens count.
+// One entry of the list: the address of a page's block of the unit's head, and in the upper 16 bits how many
+// of its tokens count.
 typedef uint64_t Fp4Entry;
 __device__ __forceinline__ Fp4Entry fp4_entry(const Fp4Params& p, int phys, int h, int tokens) {
-  return ((uint64_t)phys * p.Hkv + h) * (uint64_t)(p.tile_stride >> 4) << 8 | (uint64_t)tokens;
+  return (uint64_t)(uintptr_t)(p.pool + ((size_t)phys * p.Hkv + h) * (size_t)p.tile_stride) | (uint64_t)tokens << 48;
 }
 
-// Where fragment `frag` of the list keeps the eight tokens `oct`: the page's block and the first token's slot.
+typedef uint32_t uint4_v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2_v __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef const __attribute__((address_space(1))) unsigned char global_byte;
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(lds_byte*)p;
+}
+
+// An entry of the list by its LDS address (the compiler, which cannot tell the list from the fragments that
+// loads in flight write to LDS, would wait for those ahead of a read of its own).
+__device__ __forceinline__ uint2_v read_entry(uint32_t at) {
+  uint2_v e;
+  asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(e) : "v"(at) : "memory");
+  return e;
+}
+
+// The entry that has fragment `frag`'s tokens 8 oct .. 8 oct + 7, and their first slot in the page.
 template <int S>
-__device__ __forceinline__ const unsigned char* fp4_octet(const Fp4Params& p, const Fp4Entry* list, int frag, int oct,
-                                                          int& slot, int& tokens) {
+__device__ __forceinline__ uint32_t fp4_entry_of(uint32_t list, int frag, int oct) {
   constexpr int PPF = S < kFp4Frag ? kFp4Frag / S : 1, FPP = S > kFp4Frag ? S / kFp4Frag : 1;
-  const Fp4Entry e = list[frag / FPP * PPF + (PPF > 1 ? 8 * oct / S : 0)];
-  slot = (FPP > 1 ? kFp4Frag * (frag % FPP) : 0) + (8 * oct) % (S < kFp4Frag ? S : kFp4Frag);
-  uint32_t lo = (uint32_t)e, hi = (uint32_t)(e >> 32);
-  if (PPF == 1) {      // the same page for all lanes
-    lo = (uint32_t)uniform((int)lo);
-    hi = (uint32_t)uniform((int)hi);
-  }
-  tokens = (int)(lo & 0xffu);
-  return p.pool + ((((uint64_t)hi << 32 | (lo & ~0xffu)) >> 4));
+  return list + (PPF > 1 ? 8u * (uint32_t)(8 * oct / S) : 0u) + 8u * (uint32_t)(frag / FPP * PPF);
+}
+template <int S>
+__device__ __forceinline__ int fp4_slot(int frag, int oct) {
+  constexpr int FPP = S > kFp4Frag ? S / kFp4Frag : 1;
+  return (FPP > 1 ? kFp4Frag * (frag % FPP) : 0) + (8 * oct) % (S < kFp4Frag ? S : kFp4Frag);
 }
 
-// The keys: rows of tokens 8 (r / 4) + r % 4 and 4 on, r = lane % 16; the scales of this quarter's tokens.
+// 16 or 4 bytes a lane straight from memory to LDS, one lane's behind the other's.  (The host's pass over this
+// file does not know the wide form.)
+__device__ __forceinline__ void load_to_lds16(global_byte* src, lds_byte* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0);
+#endif
+}
+__device__ __forceinline__ void load_to_lds4(global_byte* src, lds_byte* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds(src, dst, 4, 0, 0);
+#endif
+}
+
+// Sends fragment `frag` on its way to the stage at LDS address stage_at, straight from memory: no register
+// waits for it, so a wave has several under way.  A load writes the lanes' 16 bytes one behind the other;
+// quarter a of the wave asks for the tokens 8 a .. 8 a + 7, and which lane of it for what puts the rows where
+// they are read without bank conflicts:
+//   keys    128 channels: token 8 a + 4 t + b is row 16 t + 4 a + b, its 16-byte chunk c stands at c ^ a;
+//           64 channels: token 8 a + i is row 8 a + (i ^ 4 (a % 2)), chunk c stands at c ^ (a / 2)
+//   values  the 16 bytes of lane (r, a) and channel blocks 4 i .. 4 i + 3 at 1024 i + 16 lane
+//   scales  at 64 a four words of the keys, four of the values, both once more
 template <int D, int S>
-__device__ __forceinline__ void load_fp4_keys(Fp4Frag<D>& f, const Fp4Params& p, const Fp4Entry* list, int frag) {
-  const int lane = lane_id(), r = lane & 15, kb = lane >> 4;
-  int slot, tokens;
-  const unsigned char* row = fp4_octet<S>(p, list, frag, r >> 2, slot, tokens);
-  row += (slot + (r & 3)) * (D / 2) + kb * (D / 8);
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    if constexpr (D == 128) {
-      const uint4 w = *reinterpret_cast<const uint4*>(row + 4 * t * (D / 2));
-      f.k[t][0] = w.x; f.k[t][1] = w.y; f.k[t][2] = w.z; f.k[t][3] = w.w;
-    } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(row + 4 * t * (D / 2));
-      f.k[t][0] = w.x; f.k[t][1] = w.y;
-    }
+__device__ __forceinline__ void fetch_fp4(uint32_t list, int frag, uint32_t stage_at) {
+  typedef Fp4Shape<D> Shape;
+  typedef Fp4Block<D> Block;
+  lds_byte* stage = (lds_byte*)(uintptr_t)(uint32_t)uniform((int)stage_at);
+  const int lane = lane_id(), a = lane >> 4, r = lane & 15;
+  uint2_v e = read_entry(fp4_entry_of<S>(list, frag, a));
+  if (S >= kFp4Frag) {      // the same page for all lanes
+    e.x = (uint32_t)uniform((int)e.x);
+    e.y = (uint32_t)uniform((int)e.y);
   }
-  const unsigned char* tile = fp4_octet<S>(p, list, frag, kb, slot, tokens);
-  f.ks = *reinterpret_cast<const uint4*>(tile + Fp4Block<D>::key_scales(S) + 2 * slot);
-  f.valid = tokens - slot;
-}
-
-// The values of this quarter's tokens and their scales.
-template <int D, int S>
-__device__ __forceinline__ void load_fp4_values(Fp4Frag<D>& f, const Fp4Params& p, const Fp4Entry* list, int frag) {
-  const int lane = lane_id(), r = lane & 15, kb = lane >> 4;
-  int slot, tokens;
-  const unsigned char* tile = fp4_octet<S>(p, list, frag, kb, slot, tokens);
-  const unsigned char* row = tile + Fp4Block<D>::values(S) + (slot / 8) * (4 * D) + r * 16;
+  global_byte* block = (global_byte*)((uint64_t)(e.y & 0xffffu) << 32 | e.x);
+  const int slot = fp4_slot<S>(frag, a);
+  if constexpr (D == 128) {
+    const int at = (slot + (r >> 2)) * 64 + ((lane & 3) ^ a) * 16;
+    load_to_lds16(block + at, stage + Shape::kKeys);
+    load_to_lds16(block + at + 256, stage + Shape::kKeys + 1024);
+  } else {
+    const int at = (slot + ((r >> 1) ^ (4 * (a & 1)))) * 32 + ((lane & 1) ^ (a >> 1)) * 16;
+    load_to_lds16(block + at, stage + Shape::kKeys);
+  }
+  const int v = Block::values(S) + (slot >> 3) * (4 * D) + r * 16;
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) f.v[i] = *reinterpret_cast<const uint4*>(row + 256 * i);
-  f.vs = *reinterpret_cast<const uint4*>(tile + Fp4Block<D>::value_scales(S) + 2 * slot);
+  for (int i = 0; i < D / 64; ++i) load_to_lds16(block + v + 256 * i, stage + Shape::kValues + 1024 * i);
+  const int s = ((r & 4) ? Block::value_scales(S) : Block::key_scales(S)) + 2 * slot + 4 * (r & 3);
+  load_to_lds4(block + s, stage + Shape::kScales);
 }
 
-// Running softmax state of a wave: per lane the head lane % 16.
+// Waits until all but the `kPending` loads last sent to LDS are there.
+template <int kPending>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPending) : "memory");
+}
+// Reads the keys of a stage, the scales of NV tokens and the upper half of their entry.
+template <int D, int NV>
+__device__ __forceinline__ void read_fp4_keys(uint32_t key, uint32_t second, uint32_t scale, uint32_t entry,
+                                              uint32_t (&k)[2][D / 32], uint32_t (&ks)[NV / 2], uint32_t (&vs)[NV / 2],
+                                              uint32_t& tokens) {
+  typedef typename std::conditional<D == 128, uint4_v, uint2_v>::type KeyWords;
+  typedef typename std::conditional<NV == 8, uint4_v, uint2_v>::type ScaleWords;
+  KeyWords a, b;
+  ScaleWords s, v;
+#define TS_READ_KEYS(KEY, SCALE)                                                                          \
+  asm volatile("ds_read_" KEY " %0, %5\n\tds_read_" KEY " %1, %6\n\tds_read_" SCALE " %2, %7\n\t" \
+               "ds_read_" SCALE " %3, %7 offset:16\n\tds_read_b32 %4, %8 offset:4\n\ts_waitcnt lgkmcnt(0)" \
+               : "=&v"(a), "=&v"(b), "=&v"(s), "=&v"(v), "=&v"(tokens)                                    \
+               : "v"(key), "v"(second), "v"(scale), "v"(entry)                                            \
+               : "memory")
+  if constexpr (D == 128 && NV == 8) TS_READ_KEYS("b128", "b128");
+  else if constexpr (D == 128) TS_READ_KEYS("b128", "b64");
+  else if constexpr (NV == 8) TS_READ_KEYS("b64", "b128");
+  else TS_READ_KEYS("b64", "b64");
+#undef TS_READ_KEYS
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) { k[0][i] = a[i]; k[1][i] = b[i]; }
+#pragma unroll
+  for (int i = 0; i < NV / 2; ++i) { ks[i] = s[i]; vs[i] = v[i]; }
+}
+template <int D>
+__device__ __forceinline__ void read_fp4_values(uint32_t at, uint32_t (&w)[D / 16]) {
+  if constexpr (D == 128) {
+    uint4_v a, b;
+    asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:1024\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b) : "v"(at) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { w[i] = a[i]; w[4 + i] = b[i]; }
+  } else {
+    uint4_v a;
+    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(a) : "v"(at) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = a[i];
+  }
+}
+
+// Running softmax state of a wave, for each of its sixteen columns.
 template <int D>
 struct Fp4State {
   float4_t acc[D / 16];   // channels 16 cb + 4 kb .. + 3
   float m, l;             // running maximum (log2 units, the same in the four quarters), this quarter's sum
 };
 
-// One fragment; with kMore the one behind it (next) is fetched piece by piece into the registers that this
-// one leaves: its keys go out behind the first product, its values behind the second.
-template <int D, int S, bool kMore>
-__device__ __forceinline__ void attend_fp4(Fp4State<D>& st, Fp4Frag<D>& f, const bf16x8_t (&q)[D / 32], const Fp4Params& p,
-                                           const Fp4Entry* list, int next) {
-  float s[8];
+// The fragment in the stage at LDS address `stage`.  Up to eight query heads (kNarrow) leave half of the
+// sixteen columns: they stand in both halves, and a column goes on with only one of the two logit tiles, the
+// left with the first, the right with the second: half the softmax work for each lane.  (The weights of the
+// other tile's tokens are zeros of its operand, and the halves are two partial results like two waves'.)
+// What bounds this is the vector unit: 64 of some 190 instructions expand codes (128 channels).
+template <int D, int S, bool kNarrow, bool kOut32>
+__device__ __forceinline__ void attend_fp4(Fp4State<D>& st, const bf16x8_t (&q)[D / 32], float scale_log2, uint32_t list, int frag,
+                                           uint32_t stage) {
+  typedef Fp4Shape<D> Shape;
+  constexpr int NV = kNarrow ? 4 : 8;     // logits a lane goes on with
+  const int lane = lane_id(), r = lane & 15, kb = lane >> 4, a = r >> 2, right = kNarrow ? r >> 3 : 0;
+  const uint32_t key = stage + Shape::kKeys +
+                       (D == 128 ? r * 64 + (kb ^ a) * 16
+                                 : (8 * a + (r & 3)) * 32 + ((kb >> 1) ^ (a >> 1)) * 16 + (kb & 1) * 8 + (a & 1) * 128);
+  const uint32_t second = D == 128 ? key + 1024 : key + 128 - 256 * (a & 1);     // the octet's other four tokens
+  uint32_t k[2][D / 32], ksw[NV / 2], vsw[NV / 2], tokens;
+  read_fp4_keys<D, NV>(key, second, stage + Shape::kScales + kb * 64 + right * 8, fp4_entry_of<S>(list, frag, kb), k, ksw,
+                                 vsw, tokens);
+  const int valid = (int)(tokens >> 16) - fp4_slot<S>(frag, kb) - 4 * right;
+  float s[NV], vs[NV];
   {
-    float ks[8];
-    unpack8(f.ks, ks);
+    float4_t c[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      float4_t c = {0.f, 0.f, 0.f, 0.f};
+      c[t] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_operand(f.k[t][i]), q[i], c, 0, 0, 0);
+      for (int i = 0; i < D / 32; ++i) c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_operand(k[t][i]), q[i], c[t], 0, 0, 0);
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[4 * t + i] = c[i] * (ks[4 * t + i] * p.scale_log2);
+    for (int i = 0; i < NV; ++i) {
+      const float x = kNarrow ? (right ? c[1][i] : c[0][i]) : c[i / 4][i % 4];
+      const float scale = i & 1 ? bf16_hi(ksw[i / 2]) : bf16_lo(ksw[i / 2]);
+      s[i] = x * (scale * scale_log2);
+      vs[i] = i & 1 ? bf16_hi(vsw[i / 2]) : bf16_lo(vsw[i / 2]);
     }
   }
-  const int valid = f.valid;
-  __builtin_amdgcn_sched_barrier(0);
-  if (kMore) load_fp4_keys<D, S>(f, p, list, next);
-  __builtin_amdgcn_sched_barrier(0);
-  float vs[8];
-  unpack8(f.vs, vs);
-  if (__any(valid < 8)) {   // slots without a token may hold anything, scales included
+  if (__any(valid < NV)) {   // slots without a token may hold anything, scales included
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < NV; ++i) {
       s[i] = i < valid ? s[i] : -INFINITY;
       vs[i] = i < valid ? vs[i] : 0.f;
     }
   }
   float m = s[0];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i]);
+  for (int i = 1; i < NV; ++i) m = fmaxf(m, s[i]);
   m = fmaxf(rows_max_f32(m), st.m);
   const float ref = m == -INFINITY ? 0.f : m;
   if (__any(m > st.m)) {
@@ -177,31 +262,40 @@ __device__ __forceinline__ void attend_fp4(Fp4State<D>& st, Fp4Frag<D>& f, const
     for (int cb = 0; cb < D / 16; ++cb) st.acc[cb] *= a;
     st.m = m;
   }
-  bf16x8_t hi, lo, rest;
+  uint32_t w[D / 16];
+  read_fp4_values<D>(stage + Shape::kValues + 16 * lane, w);
+  // the weights as two bf16 numbers, three where the output is fp32: pairs in a word
+  constexpr int kTerms = kOut32 ? 3 : 2;
+  uint32_t part[kTerms][NV / 2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float w = __builtin_amdgcn_exp2f(s[i] - ref);
-    st.l += w;
-    const float x = w * vs[i];
-    hi[i] = (__bf16)x;
-    const float y = x - (float)hi[i];
-    lo[i] = (__bf16)y;
-    rest[i] = (__bf16)(y - (float)lo[i]);
+  for (int i = 0; i < NV; i += 2) {
+    const float w0 = __builtin_amdgcn_exp2f(s[i] - ref), w1 = __builtin_amdgcn_exp2f(s[i + 1] - ref);
+    st.l += w0 + w1;
+    float x0 = w0 * vs[i], x1 = w1 * vs[i + 1];
+#pragma unroll
+    for (int e = 0; e < kTerms; ++e) {
+      const uint32_t pair = pack_elems<false>(x0, x1);
+      part[e][i / 2] = pair;
+      x0 -= bf16_lo(pair);
+      x1 -= bf16_hi(pair);
+    }
   }
-  auto word = [&](int cb) {
-    const uint4 w = f.v[cb / 4];
-    return cb % 4 == 0 ? w.x : cb % 4 == 1 ? w.y : cb % 4 == 2 ? w.z : w.w;
-  };
+  bf16x8_t term[kTerms];
+  const uint32_t left_on = kNarrow && right ? 0u : ~0u;
+#pragma unroll
+  for (int e = 0; e < kTerms; ++e) {
+    uint4_v o;
+    if constexpr (kNarrow)
+      o = uint4_v{part[e][0] & left_on, part[e][1] & left_on, part[e][0] & ~left_on, part[e][1] & ~left_on};
+    else o = uint4_v{part[e][0], part[e][1], part[e][NV / 2 - 2], part[e][NV / 2 - 1]};
+    term[e] = __builtin_bit_cast(bf16x8_t, o);
+  }
 #pragma unroll
   for (int cb = 0; cb < D / 16; ++cb) {
-    const bf16x8_t v = fp4_operand(word(cb));
-    st.acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, rest, st.acc[cb], 0, 0, 0);
-    st.acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, st.acc[cb], 0, 0, 0);
-    st.acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, st.acc[cb], 0, 0, 0);
+    const bf16x8_t v = fp4_operand(w[cb]);
+#pragma unroll
+    for (int e = kTerms - 1; e >= 0; --e) st.acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, term[e], st.acc[cb], 0, 0, 0);
   }
-  __builtin_amdgcn_sched_barrier(0);
-  if (kMore) load_fp4_values<D, S>(f, p, list, next);
-  __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int S, bool kSparse>
@@ -219,15 +313,19 @@ __device__ __forceinline__ void store_fp4_out(const Fp4Params& p, size_t idx, fl
   else p.out[idx] = v;
 }
 
-template <int D, int S, bool kSparse>
-__global__ __launch_bounds__(Fp4Shape<D>::kThreadsPer, Fp4Shape<D>::kOccupancy) void fp4_attention_kernel(Fp4Params p) {
-  constexpr int kFp4Waves = Fp4Shape<D>::kWavesPer, kFp4Threads = Fp4Shape<D>::kThreadsPer;
+template <int D, int S, bool kSparse, bool kNarrow, bool kOut32>
+__global__ __launch_bounds__(Fp4Shape<D>::kThreadsPer, Fp4Shape<D>::kPerCu * Fp4Shape<D>::kWavesPer / 4)
+void fp4_attention_kernel(Fp4Params p) {
+  typedef Fp4Shape<D> Shape;
+  constexpr int kFp4Waves = Shape::kWavesPer, kFp4Threads = Shape::kThreadsPer, kStages = Shape::kStages;
   constexpr int PPF = S < kFp4Frag ? kFp4Frag / S : 1, FPP = S > kFp4Frag ? S / kFp4Frag : 1;
   constexpr int kFrags = (kFp4List + 1 - FPP) * FPP / PPF;   // fragments the list in LDS covers, begun within a page too
   constexpr int kRow = D + 4;                        // a head's merged row: channels, maximum, sum
+  constexpr int kWaveRows = Shape::kRing / 4;        // a wave's rows lie where its fragments were
+  static_assert(16 * kRow <= kWaveRows, "room for a wave's rows");
   extern __shared__ __align__(16) unsigned char smem[];
   Fp4Entry* list = reinterpret_cast<Fp4Entry*>(smem);
-  float* merge = reinterpret_cast<float*>(list + kFp4List);       // [waves][G][kRow]
+  float* merge = reinterpret_cast<float*>(list + kFp4List);
   __shared__ int last_one;
   const int tid = threadIdx.x, lane = lane_id(), wave = wave_id(), r = lane & 15, kb = lane >> 4;
 
@@ -284,11 +382,12 @@ __global__ __launch_bounds__(Fp4Shape<D>::kThreadsPer, Fp4Shape<D>::kOccupancy) 
     const int u = b * p.Hkv + h;
     const int len = min(max(p.seq_lens[b], 0), p.Pmax * S), count = kSparse ? min(max(p.sel_count[b], 0), p.Kmax) : 0;
     bf16x8_t q[D / 32];
+    const int head = kNarrow ? r & 7 : r;      // of this lane's column
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      const uint16_t* src = p.q + ((size_t)b * p.Hq + h * p.G + min(r, p.G - 1)) * D + kb * (D / 4) + 8 * i;
+      const uint16_t* src = p.q + ((size_t)b * p.Hq + h * p.G + min(head, p.G - 1)) * D + kb * (D / 4) + 8 * i;
       uint4 w = *reinterpret_cast<const uint4*>(src);
-      if (r >= p.G) w = make_uint4(0u, 0u, 0u, 0u);
+      if (head >= p.G) w = make_uint4(0u, 0u, 0u, 0u);
       q[i] = __builtin_bit_cast(bf16x8_t, w);
     }
     Fp4State<D> st;
@@ -313,19 +412,29 @@ __global__ __launch_bounds__(Fp4Shape<D>::kThreadsPer, Fp4Shape<D>::kOccupancy) 
       }
       __syncthreads();
       const int shift = c0 % FPP - c0;      // fragments as the list has them
-      if (c0 + wave < c1) {
-        Fp4Frag<D> fr;
-        int f = c0 + wave + shift;
-        load_fp4_keys<D, S>(fr, p, list, f);
-        load_fp4_values<D, S>(fr, p, list, f);
-        for (; f + kFp4Waves < c1 + shift; f += kFp4Waves) attend_fp4<D, S, true>(st, fr, q, p, list, f + kFp4Waves);
-        attend_fp4<D, S, false>(st, fr, q, p, list, 0);
+      const uint32_t list_at = lds_address(list), ring = lds_address(merge) + wave * Shape::kRing;
+      const int last = c1 + shift;
+      int f = c0 + wave + shift, stage = 0;
+#pragma unroll
+      for (int i = 0; i < kStages - 1; ++i)
+        if (f + i * kFp4Waves < last) fetch_fp4<D, S>(list_at, f + i * kFp4Waves, ring + i * Shape::kStage);
+      for (; f < last; f += kFp4Waves) {
+        const int ahead = f + (kStages - 1) * kFp4Waves;
+        const int to = stage == 0 ? kStages - 1 : stage - 1;      // the stage that the fragment before has left
+        if (ahead < last) {
+          fetch_fp4<D, S>(list_at, ahead, ring + to * Shape::kStage);
+          wait_loads<(kStages - 1) * Shape::kLoads>();
+        } else {
+          wait_loads<0>();
+        }
+        attend_fp4<D, S, kNarrow, kOut32>(st, q, p.scale_log2, list_at, f, ring + stage * Shape::kStage);
+        stage = stage == kStages - 1 ? 0 : stage + 1;
       }
     }
     // the waves' results: head rows of channels, maximum, sum
     const float l = rows_sum_f32(st.l);
-    if (r < p.G) {
-      float* row = merge + (wave * p.G + r) * kRow;
+    if (head < p.G) {
+      float* row = merge + wave * kWaveRows + r * kRow;
 #pragma unroll
       for (int cb = 0; cb < D / 16; ++cb) *reinterpret_cast<float4_t*>(row + 16 * cb + 4 * kb) = st.acc[cb];
       if (kb == 0) {
@@ -340,23 +449,24 @@ __global__ __launch_bounds__(Fp4Shape<D>::kThreadsPer, Fp4Shape<D>::kOccupancy) 
     float* mine = p.part + ((size_t)blockIdx.x * 2 + (at > ustart ? 0 : 1)) * p.G * (D + 2);
     for (int i = tid; i < p.G * D; i += kFp4Threads) {
       const int g = i / D, c = i % D;
+      constexpr int kHalves = kNarrow ? 2 : 1;       // columns of a head
       float M = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kFp4Waves; ++w) M = fmaxf(M, merge[(w * p.G + g) * kRow + D]);
+      for (int w = 0; w < kFp4Waves * kHalves; ++w) M = fmaxf(M, merge[w / kHalves * kWaveRows + (g + w % kHalves * 8) * kRow + D]);
       float o = 0.f, sum = 0.f;
       if (M != -INFINITY) {
 #pragma unroll
-        for (int w = 0; w < kFp4Waves; ++w) {
-          const float* row = merge + (w * p.G + g) * kRow;
+        for (int w = 0; w < kFp4Waves * kHalves; ++w) {
+          const float* row = merge + w / kHalves * kWaveRows + (g + w % kHalves * 8) * kRow;
           const float a = __builtin_amdgcn_exp2f(row[D] - M);
           o += a * row[c];
           sum += a * row[D + 1];
         }
       }
       if (whole) {
-        const size_t head = (size_t)b * p.Hq + h * p.G + g;
-        store_fp4_out(p, head * D + c, sum > 0.f ? o / sum : 0.f);
-        if (p.lse && c == 0) p.lse[head] = sum > 0.f ? (M + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        const size_t at_head = (size_t)b * p.Hq + h * p.G + g;
+        store_fp4_out(p, at_head * D + c, sum > 0.f ? o / sum : 0.f);
+        if (p.lse && c == 0) p.lse[at_head] = sum > 0.f ? (M + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
       } else {
         store_agent(mine + g * (D + 2) + c, o);
         if (c == 0) {
@@ -412,9 +522,9 @@ __global__ __launch_bounds__(Fp4Shape<D>::kThreadsPer, Fp4Shape<D>::kOccupancy) 
               }
             }
           }
-          const size_t head = (size_t)b * p.Hq + h * p.G + g;
-          store_fp4_out(p, head * D + c, sum > 0.f ? o / sum : 0.f);
-          if (p.lse && c == 0) p.lse[head] = sum > 0.f ? (M + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
+          const size_t at_head = (size_t)b * p.Hq + h * p.G + g;
+          store_fp4_out(p, at_head * D + c, sum > 0.f ? o / sum : 0.f);
+          if (p.lse && c == 0) p.lse[at_head] = sum > 0.f ? (M + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
         }
       }
     }
