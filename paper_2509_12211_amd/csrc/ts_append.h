@@ -23,37 +23,23 @@ constexpr int kPoolBf16 = 0, kPoolInt8 = 1, kPoolFp16 = 2, kPoolFp4 = 3;
 // has at most ten significant bits: exact in fp32.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float fp4_row_scale(float amax) {
-  if (!(amax > 0.f)) return 1.0f;
-  const uint32_t b = __float_as_uint(__fdiv_rn(fminf(amax, FLT_MAX), 6.0f));
-  return __uint_as_float((b + 0xffffu) & 0xffff0000u);
+  const uint32_t b = __float_as_uint(__fdiv_rn(amax, 6.0f));
+  return amax > 0.f ? __uint_as_float((b + 0xffffu) & 0xffff0000u) : 1.0f;
 }
 typedef float float2_t __attribute__((ext_vector_type(2)));
-// The codes of eight numbers of a row, four bits each: the nearest, ties to the even code, no negative zero; NaN
-// is 0.  The quotient is the reciprocal's product corrected by its remainder: exact where x / scale is a
-// number's border (a tie), and elsewhere off by far less than the 2^-11 that eight-bit numbers keep away from
-// one.  Rows of very small or large scale are moved to the middle of the range first (exactly).
-struct Fp4Quotient {
-  float f, s, r;
-  __device__ __forceinline__ explicit Fp4Quotient(float scale) {
-    f = scale < 0x1p-60f ? 0x1p100f : scale > 0x1p60f ? 0x1p-100f : 1.0f;
-    s = scale * f;
-    r = __builtin_amdgcn_rcpf(s);
-  }
-  __device__ __forceinline__ float operator()(float x) const {
-    x *= f;
-    const float q = x * r;
-    const float z = fmaf(fmaf(-q, s, x), r, q);
-    return fminf(fmaxf(z, -6.0f), 6.0f);
-  }
-};
+// The codes of eight numbers of a row, four bits each: the nearest, ties to the even code, no negative zero.  The
+// quotient is the reciprocal's product corrected by its remainder: exact where x / scale is a number's border
+// (a tie), and elsewhere off by far less than the 2^-11 that eight-bit numbers keep away from one.  kFar: rows of
+// very small or large scale are moved to the middle of the range first (exactly).
+template <bool kFar>
 __device__ __forceinline__ uint32_t fp4_codes(const float (&x)[8], float scale) {
-  const Fp4Quotient quotient(scale);
+  const float f = !kFar ? 1.0f : scale < 0x1p-60f ? 0x1p100f : scale > 0x1p60f ? 0x1p-100f : 1.0f;
+  const float s = kFar ? scale * f : scale, r = __builtin_amdgcn_rcpf(s);
   float z[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    // infinities saturate, NaN is 0
-    const float y = fminf(fmaxf(x[i], -FLT_MAX), FLT_MAX);
-    z[i] = x[i] == x[i] ? quotient(y) : 0.f;
+    const float y = kFar ? x[i] * f : x[i], q = y * r;
+    z[i] = fmaf(fmaf(-q, s, y), r, q);
   }
   uint32_t w = 0u;
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, z[0], z[1], 1.0f, 0);
@@ -113,12 +99,27 @@ struct AppendParams {
 template <int FMT, int D>
 struct AppendLds {
   typedef typename std::conditional<FMT == kPoolInt8 || FMT == kPoolFp4, uint8_t, uint16_t>::type Elem;
-  static constexpr int kRow = D + 8;   // elements of a staged row of values
-  static constexpr int kWavesPer = kRotaryThreads / kWave;
+  static constexpr bool kWide = sizeof(Elem) == 2;
+  static constexpr int kRow = D + 8;   // elements of a staged row
+  // partial boxes: of each wave, or with 16 bits of as many threads as there are for each pair of channels
+  static constexpr int kParts = kWide ? 2 * kRotaryThreads / D : kRotaryThreads / kWave;
   __host__ __device__ static constexpr size_t bytes(int S) {
-    return (size_t)S * kRow * sizeof(Elem) + 2 * (size_t)kWavesPer * D * 4;
+    return (kWide ? 2 : 1) * (size_t)S * kRow * sizeof(Elem) + 2 * (size_t)kParts * D * 4;
   }
 };
+
+// Minimum and maximum as the instruction has them: a NaN gives way to the other number.  (fminf and fmaxf
+// quieten their operands with an instruction each first.)
+__device__ __forceinline__ float raw_min(float a, float b) {
+  float r;
+  asm("v_min_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ float raw_max(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
 
 // A row as the cache stores it: 16 bits (two chunks of four), eight int8 codes, or eight 4-bit codes.
 struct StoredRow {
@@ -132,11 +133,11 @@ __device__ __forceinline__ StoredRow store_form(uint2 x, uint2 y) {
   s.b = y;
   s.scale = 1.f;
   if constexpr (FMT == kPoolInt8 || FMT == kPoolFp4) {
-    const float f[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y),
-                        bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
+    float f[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y),
+                  bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
     float amax = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(f[i]));
+    for (int i = 0; i < 8; ++i) amax = raw_max(amax, fabsf(f[i]));
     amax = group_max_f32<D / 8>(amax);
     if constexpr (FMT == kPoolInt8) {
       s.scale = i8_row_scale(amax);
@@ -146,8 +147,16 @@ __device__ __forceinline__ StoredRow store_form(uint2 x, uint2 y) {
       s.a.x = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
       s.b.x = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
     } else {
+      bool odd = false;      // (a NaN is no maximum: it is looked for by itself)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) odd |= !(fabsf(f[i]) <= FLT_MAX);
+      if (__any(odd)) {      // infinities are the largest number of their row's scale, NaN is 0
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = f[i] == f[i] ? fminf(fmaxf(f[i], -FLT_MAX), FLT_MAX) : 0.f;
+        amax = fminf(amax, FLT_MAX);
+      }
       s.scale = fp4_row_scale(amax);
-      s.a.x = fp4_codes(f, s.scale);
+      s.a.x = __any(s.scale < 0x1p-60f || s.scale > 0x1p60f) ? fp4_codes<true>(f, s.scale) : fp4_codes<false>(f, s.scale);
     }
   }
   return s;
@@ -349,7 +358,7 @@ __device__ __forceinline__ bool find_page(const AppendParams& p, int sh, int tas
 // Minimum or maximum of a value over the lanes of the wave that hold the same channels.
 template <int LPR, bool kMax>
 __device__ __forceinline__ float over_groups(float v) {
-  auto take = [](float x, float y) { return kMax ? fmaxf(x, y) : fminf(x, y); };
+  auto take = [](float x, float y) { return kMax ? raw_max(x, y) : raw_min(x, y); };
   if (LPR == 8)
     v = take(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), kDppRowRor8, 0xf, 0xf, true)));
   uint2s_t r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -359,9 +368,10 @@ __device__ __forceinline__ float over_groups(float v) {
 }
 
 // grid (touched pages or more, Hkv).  A token's key, value and queries are dealt to as many groups of
-// lanes as the workgroup has for each token, the rows asked for ahead of the lookups.  The extremes of the
-// keys as stored stay in the registers of the lanes that hold their channels, and meet over the wave's
-// groups and then, in LDS, over the waves.
+// lanes as the workgroup has for each token, the rows asked for ahead of the lookups.  Half of the time goes to
+// the vector unit (some hundred instructions a row), so the box is worked out where that takes the fewest: with
+// 16 bits from the keys in LDS, two channels a thread; quantised, from the numbers that the lanes hold anyway, over
+// the wave's groups and then, in LDS, over the waves.
 template <int FMT, int D>
 __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendParams p) {
   constexpr bool kHalf = FMT == kPoolFp16;
@@ -370,7 +380,8 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
   typedef typename Lds::Elem Elem;
   extern __shared__ __align__(16) unsigned char smem[];
   Elem* vs = reinterpret_cast<Elem*>(smem);                                                  // [S][kRow]
-  float* box = reinterpret_cast<float*>(smem + (size_t)p.S * Lds::kRow * sizeof(Elem));      // [2][waves][D]
+  Elem* ks = Lds::kWide ? vs + (size_t)p.S * Lds::kRow : vs;                                 // 16 bits: [S][kRow]
+  float* box = reinterpret_cast<float*>(ks + (size_t)p.S * Lds::kRow);                       // [2][parts][D]
   const int sh = __builtin_ctz(p.S), h = blockIdx.y, tid = threadIdx.x;
   int b, j;
   if (!find_page(p, sh, blockIdx.x, b, j)) return;
@@ -378,7 +389,7 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
   const int len = uniform(p.seq_lens[b] - (p.lens_after ? p.cu[b + 1] - p.cu[b] : 0));
   if (len < 0) return;                                   // (no such length)
   const int p0 = max(j << sh, len), p1 = min((j + 1) << sh, len + n);   // positions of this page's new tokens
-  const int ntok = p1 - p0, slot0 = p0 - (j << sh), tok0 = c0 + p0 - len;
+  const int ntok = uniform(p1 - p0), slot0 = p0 - (j << sh), tok0 = c0 + p0 - len;
   const bool fits = (long long)len + n <= (long long)p.Pmax << sh;
   const int phys = uniform(fits ? p.block_table[(size_t)b * p.Pmax + j] : -1);
   const bool store = phys >= 0 && phys < p.n_phys;
@@ -391,7 +402,7 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
   load_norm(p.r.q_norm, lanes.c0, lanes.c1, qn);
   load_norm(p.r.k_norm, lanes.c0, lanes.c1, kn);
   const bool has_k = store && part == 0, has_v = store && part == (step > 1 ? 1 : 0);
-  const int G = p.q != nullptr ? p.G : 0;
+  const int G = p.q != nullptr ? p.G : 0, rounds = (G + step - 1) / step;
   const int g0 = step > 2 ? (part + step - 2) % step : part;          // queries go to the groups behind first
   float lo[8], hi[8];
 #pragma unroll
@@ -401,12 +412,14 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
     constexpr int kAhead = 4;
     const uint16_t* q_src = p.q + tok * p.q_stride + (size_t)h * p.G * D;
     uint2 qa[kAhead], qb[kAhead], ka, kb, va, vb;
-    auto fetch = [&](int g) {
+    // (the number of rounds is the same for all: a group without a row in the last one fetches another's)
+    auto fetch = [&](int round) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
-        if (g + i * step < G) {
-          qa[i] = *reinterpret_cast<const uint2*>(q_src + (g + i * step) * D + lanes.c0);
-          qb[i] = *reinterpret_cast<const uint2*>(q_src + (g + i * step) * D + lanes.c1);
+        if (round + i < rounds) {
+          const uint16_t* src = q_src + min(g0 + (round + i) * step, G - 1) * D;
+          qa[i] = *reinterpret_cast<const uint2*>(src + lanes.c0);
+          qb[i] = *reinterpret_cast<const uint2*>(src + lanes.c1);
         }
     };
     if (has_k) {
@@ -419,7 +432,7 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
       va = *reinterpret_cast<const uint2*>(src);
       vb = *reinterpret_cast<const uint2*>(src + 4);
     }
-    fetch(g0);
+    fetch(0);
     Angles ang;
     load_angles(p.r, li, lanes.turns,
                 [&](int axis) { return p.r.positions ? p.r.positions[(size_t)axis * p.r.T + tok] : p0 + i0; }, ang);
@@ -427,12 +440,17 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
       rotate_row<D, kHalf>(p.r, lanes.turns, kn, ang, ka, kb);
       const StoredRow s = store_form<FMT, D>(ka, kb);
       store_key<FMT, D>(p, tile.k, tile.scale_row, slot, lanes.c0, lanes.c1, li, s);
-      float l[8], u[8];
-      stored_numbers<FMT>(s, l, u);
+      if constexpr (Lds::kWide) {
+        *reinterpret_cast<uint2*>(ks + slot * Lds::kRow + lanes.c0) = s.a;
+        *reinterpret_cast<uint2*>(ks + slot * Lds::kRow + lanes.c1) = s.b;
+      } else {
+        float l[8], u[8];
+        stored_numbers<FMT>(s, l, u);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        lo[i] = fminf(lo[i], l[i]);
-        hi[i] = fmaxf(hi[i], u[i]);
+        for (int i = 0; i < 8; ++i) {
+          lo[i] = raw_min(lo[i], l[i]);
+          hi[i] = raw_max(hi[i], u[i]);
+        }
       }
     }
     if (has_v) {
@@ -451,47 +469,64 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
       if (li == 0) store_value_scale<FMT, D>(p, tile.k, tile.scale_row, slot, s.scale);
     }
     uint16_t* q_dst = p.q_out + tok * p.q_out_stride + (size_t)h * p.G * D;
-    for (int g = g0; g < G;) {
+    for (int round = 0; round < rounds;) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
-        if (g + i * step < G) {
+        if (round + i < rounds) {
           rotate_row<D, kHalf>(p.r, lanes.turns, qn, ang, qa[i], qb[i]);
-          *reinterpret_cast<uint2*>(q_dst + (g + i * step) * D + lanes.c0) = qa[i];
-          *reinterpret_cast<uint2*>(q_dst + (g + i * step) * D + lanes.c1) = qb[i];
+          const int g = g0 + (round + i) * step;
+          if (g < G) {
+            *reinterpret_cast<uint2*>(q_dst + g * D + lanes.c0) = qa[i];
+            *reinterpret_cast<uint2*>(q_dst + g * D + lanes.c1) = qb[i];
+          }
         }
-      g += kAhead * step;
-      fetch(g);
+      round += kAhead;
+      fetch(round);
     }
   }
   if (!store) return;
+  const int slot1 = slot0 + ntok;
+  if constexpr (Lds::kWide) {
+    __syncthreads();
+    const int pair = tid % (D / 2), part = tid / (D / 2);
+    float l0 = INFINITY, l1 = INFINITY, u0 = -INFINITY, u1 = -INFINITY;
+    for (int s = slot0 + part; s < slot1; s += Lds::kParts) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(ks + s * Lds::kRow + 2 * pair);
+      const float x = elem_lo<kHalf>(w), y = elem_hi<kHalf>(w);
+      l0 = raw_min(l0, x); u0 = raw_max(u0, x);
+      l1 = raw_min(l1, y); u1 = raw_max(u1, y);
+    }
+    *reinterpret_cast<float2*>(box + part * D + 2 * pair) = make_float2(l0, l1);
+    *reinterpret_cast<float2*>(box + (Lds::kParts + part) * D + 2 * pair) = make_float2(u0, u1);
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo[i] = over_groups<LPR, false>(lo[i]);
-    hi[i] = over_groups<LPR, true>(hi[i]);
-  }
-  if (lane_id() < LPR) {
-    float* mine = box + wave_id() * D;
+    for (int i = 0; i < 8; ++i) {
+      lo[i] = over_groups<LPR, false>(lo[i]);
+      hi[i] = over_groups<LPR, true>(hi[i]);
+    }
+    if (lane_id() < LPR) {
+      float* mine = box + wave_id() * D;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      mine[lanes.c0 + i] = lo[i];
-      mine[lanes.c1 + i] = lo[4 + i];
-      mine[Lds::kWavesPer * D + lanes.c0 + i] = hi[i];
-      mine[Lds::kWavesPer * D + lanes.c1 + i] = hi[4 + i];
+      for (int i = 0; i < 4; ++i) {
+        mine[lanes.c0 + i] = lo[i];
+        mine[lanes.c1 + i] = lo[4 + i];
+        mine[Lds::kParts * D + lanes.c0 + i] = hi[i];
+        mine[Lds::kParts * D + lanes.c1 + i] = hi[4 + i];
+      }
     }
   }
   __syncthreads();
-  const int slot1 = slot0 + ntok;
   if (tid < D) {
-    float l = box[tid], u = box[Lds::kWavesPer * D + tid];
+    float l = box[tid], u = box[Lds::kParts * D + tid];
 #pragma unroll
-    for (int i = 1; i < Lds::kWavesPer; ++i) {
-      l = fminf(l, box[i * D + tid]);
-      u = fmaxf(u, box[(Lds::kWavesPer + i) * D + tid]);
+    for (int i = 1; i < Lds::kParts; ++i) {
+      l = raw_min(l, box[i * D + tid]);
+      u = raw_max(u, box[(Lds::kParts + i) * D + tid]);
     }
     const size_t at = (((size_t)b * p.Hkv + h) * p.Pmax + j) * D + tid;
     if (slot0 != 0) {
-      l = fminf(l, elem_to_f32<kHalf>(p.page_min[at]));
-      u = fmaxf(u, elem_to_f32<kHalf>(p.page_max[at]));
+      l = raw_min(l, elem_to_f32<kHalf>(p.page_min[at]));
+      u = raw_max(u, elem_to_f32<kHalf>(p.page_max[at]));
     }
     p.page_min[at] = box_number<FMT>(l, false);
     p.page_max[at] = box_number<FMT>(u, true);
@@ -501,17 +536,14 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
     const int oct0 = slot0 >> 3, octs = ((slot1 + 7) >> 3) - oct0;
     for (int i = tid; i < octs * D; i += kRotaryThreads) {
       const int o = oct0 + i / D, w = i % D, ch = Fp4Block<D>::channel(w);
-      uint32_t word = 0u, mask = 0u;
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int s = 8 * o + t;
-        if (s >= slot0 && s < slot1) {
-          word |= (uint32_t)vs[s * Lds::kRow + ch] << (4 * t);
-          mask |= 15u << (4 * t);
-        }
-      }
       uint32_t* dst = reinterpret_cast<uint32_t*>(tile.v) + (size_t)o * D + w;
-      *dst = mask == 0xffffffffu ? word : (*dst & ~mask) | word;
+      // (slots without a new token hold anything: their codes are masked)
+      uint32_t word = 0u;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) word |= (uint32_t)(vs[(8 * o + t) * Lds::kRow + ch] & 15u) << (4 * t);
+      const int from = max(slot0 - 8 * o, 0), upto = min(slot1 - 8 * o, 8);
+      const uint32_t mask = (upto == 8 ? 0xffffffffu : (1u << (4 * upto)) - 1u) & ~((1u << (4 * from)) - 1u);
+      *dst = mask == 0xffffffffu ? word : (*dst & ~mask) | (word & mask);
     }
   } else {
     constexpr int kMost = 16 / (int)sizeof(Elem);      // tokens in 16 bytes
