@@ -182,6 +182,7 @@ __global__ __launch_bounds__(kThreads) void score_pages_kernel(const uint16_t* q
                                                                const int32_t* seq_lens, float* scores,
                                                                int G, uint32_t magic_hkv, int S, int Pmax) {
   __shared__ __align__(16) unsigned char q_stage[ScoreLanes<D, kHalf>::query_stage_bytes(16)];
+  TS_MARK_INIT();
   const int u = blockIdx.y, b = fast_div(u, FastDiv{1, magic_hkv});
   float* srow = scores + (size_t)u * Pmax;
   const uint16_t *pmin_u = page_min + (size_t)u * Pmax * D, *pmax_u = page_max + (size_t)u * Pmax * D;
