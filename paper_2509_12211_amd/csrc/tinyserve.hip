@@ -377,7 +377,7 @@ static AttendParams attend_params(const ts_layout* L, const Plan& pl, const void
 // The 4-bit cache
 // ---------------------------------------------------------------------------
 struct Fp4Plan {
-  int workgroups;
+  int workgroups, room;   // of the launch; of those that may share a unit
   size_t off_done, off_part, attend_total, off_scores, off_sel, off_count, total;
 };
 
@@ -391,12 +391,13 @@ static Fp4Plan make_fp4_plan(const ts_layout* L, int pages, bool query_aware) {
   const int share = d64 ? Fp4Shape<64>::kMinShare : Fp4Shape<128>::kMinShare;
   const int resident = d64 ? Fp4Shape<64>::kResident : Fp4Shape<128>::kResident;
   const long long most = (frags + share - 1) / share;
-  pl.workgroups = most < resident ? (int)most : resident;
+  pl.room = most < resident ? (int)most : resident;
+  pl.workgroups = pl.room > units ? pl.room : units;
   size_t off = kCtrlArea * sizeof(int32_t);
   pl.off_done = off;
   off = align_up(off + (size_t)units * sizeof(int32_t), 256);
   pl.off_part = off;
-  off = align_up(off + (size_t)pl.workgroups * 2 * G * (L->head_dim + 2) * sizeof(float), 256);
+  off = align_up(off + (size_t)pl.room * 2 * G * (L->head_dim + 2) * sizeof(float), 256);
   pl.attend_total = off;
   pl.off_scores = off;
   if (query_aware) off = align_up(off + (size_t)units * L->max_pages_per_seq * sizeof(float), 256);
@@ -430,6 +431,8 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
   p.Kmax = Kmax;
   p.n_phys = L->num_phys_pages;
   p.out_bf16 = L->out_format == TS_OUT_BF16;
+  p.room = pl.room;
+  p.inv_room = 1.0f / (float)pl.room;
   p.tile_stride = tile_stride_of(L);
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
   int st = TS_OK;

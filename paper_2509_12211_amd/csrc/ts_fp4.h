@@ -12,9 +12,10 @@
 // Row 4 kb + i of logit tile t is token 8 kb + 4 t + i of the fragment (kb: quarter of the wave), so the eight
 // weights a lane has are the eight tokens its quarter contracts in the second product.
 //
-// Work: the units' fragments are numbered through, unit after unit, and every workgroup takes an equal
-// contiguous share, whatever the lengths; each works out from the lengths which.  A workgroup's waves take
-// the fragments of a unit in turn and merge in LDS.  A unit that several workgroups share is merged by the
+// Work: every workgroup works out from the lengths what it has to do.  Much work is numbered through, fragment
+// after fragment and unit after unit, and dealt out in equal contiguous shares, whatever the lengths; little goes
+// unit by unit, each to as many workgroups as its length asks for.  A workgroup's waves take the fragments of a
+// unit in turn and merge in LDS.  A unit that several workgroups share is merged by the
 // last of them to arrive (an atomic count in the workspace, set back to zero); nobody waits.
 #pragma once
 #include "ts_append.h"
@@ -25,6 +26,7 @@ namespace ts {
 constexpr int kFp4Frag = 32;            // tokens of a fragment
 constexpr int kFp4List = 1024;          // list entries held in LDS at a time
 constexpr int kFp4Parts = 64;           // about how many workgroups share a unit at the most
+constexpr uint32_t kFp4LongShare = 192; // fragments of a workgroup from which on all get the same number
 
 // Workgroups of eight waves, two on a compute unit, for 64 channels; with 128, where a wave's registers leave
 // room for three on a SIMD and no less, of four, three on a unit (ragged batch of 1.1 GB 232 -> 223 us, lists of
@@ -35,7 +37,7 @@ struct Fp4Shape {
   static constexpr int kPerCu = D == 64 ? 2 : 3;              // workgroups on a compute unit
   static constexpr int kStages = D == 64 ? 3 : 2;             // fragments a wave has room for
   static constexpr int kResident = 256 * kPerCu;
-  static constexpr int kMinShare = 2 * kWavesPer;             // fragments a workgroup has at the least
+  static constexpr int kMinShare = 16;                        // fragments a workgroup has at the least
   // a fragment in LDS: keys, values, scales
   static constexpr int kKeys = 0, kValues = 16 * D, kScales = 32 * D, kStage = 32 * D + 256;
   static constexpr int kLoads = D / 32 + 1;                   // loads that bring it
@@ -53,11 +55,12 @@ struct Fp4Params {
   const int32_t *sel, *sel_count;   // sparse: [B][Hkv][Kmax], [B]
   float* out;                       // [B][Hq][D] fp32 or bf16
   float* lse;                       // nullable [B][Hq]
-  float* part;                      // [workgroups][2][G][D + 2]: what a unit's workgroups hand over
+  float* part;                      // [room][2][G][D + 2]: what a unit's workgroups hand over
   int32_t* done;                    // [units] workgroups that have; zero between launches
   int B, Hq, Hkv, G, Pmax, Kmax, n_phys, out_bf16;
+  int room;                         // workgroups that have a place in part, and are at work at once
   long long tile_stride;
-  float scale_log2;
+  float scale_log2, inv_room;
 };
 
 // Eight codes, two a byte, as an operand of eight bf16 numbers.
@@ -298,6 +301,12 @@ __device__ __forceinline__ void attend_fp4(Fp4State<D>& st, const bf16x8_t (&q)[
   }
 }
 
+// n / d for n < 2^20: the fraction that half a unit adds (0.5 / d) outweighs what the reciprocal is off (2^-22 n / d).
+// (A division proper takes some forty instructions, ahead of the first load.)
+__device__ __forceinline__ uint32_t small_quotient(uint32_t n, uint32_t d) {
+  return (uint32_t)(((float)n + 0.5f) * __builtin_amdgcn_rcpf((float)d));
+}
+
 template <int S, bool kSparse>
 __device__ __forceinline__ int fp4_frags(const Fp4Params& p, int b) {
   if (kSparse) {
@@ -351,31 +360,71 @@ void fp4_attention_kernel(Fp4Params p) {
     }
   }
   total *= (uint32_t)p.Hkv;
-  const uint32_t share = max(max((uint32_t)Fp4Shape<D>::kMinShare, (total + gridDim.x - 1) / gridDim.x),
-                             (uint32_t)((longest + kFp4Parts - 1) / kFp4Parts));
-  uint32_t at = blockIdx.x * share;
-  const uint32_t end = min(total, at + share);
-  if (at >= end) return;
-  int b = 0, nf = 0;
-  uint32_t ustart = 0;    // first fragment of the unit
-  for (int base = 0, before = 0; base < p.B; base += kWave) {
-    if (p.B > kWave) {      // (up to 64 sequences the lanes have them still)
-      mine = base + lane < p.B ? fp4_frags<S, kSparse>(p, base + lane) : 0;
-      upto = before + wave_inclusive_sum(mine);
+  const uint32_t floor_share = max((uint32_t)Shape::kMinShare, (uint32_t)((longest + kFp4Parts - 1) / kFp4Parts));
+  const uint32_t room = (uint32_t)p.room, units = (uint32_t)p.B * (uint32_t)p.Hkv;
+  // (no less than total / room: up to 4 M fragments a workgroup the rounding of the quotient is below the one added)
+  uint32_t share = max(floor_share, (uint32_t)((float)total * p.inv_room) + 1u);
+  // Workgroups of a unit each, or equal shares of all fragments?  A workgroup whose share reaches into a second
+  // unit begins once more, which takes as long as a hundred fragments: short shares go unit by unit wherever
+  // there are workgroups for that at once (one sequence of 3000 tokens, four heads: 12.9 -> 8.7 us).
+  auto by_units = [&](uint32_t s) {       // workgroups that units in parts of at most s take
+    uint32_t n = 0;
+    for (int base = 0; base < p.B; base += kWave) {
+      const int i = base + lane, f = p.B <= kWave ? mine : i < p.B ? fp4_frags<S, kSparse>(p, i) : 0;
+      n += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_sum((int)small_quotient((uint32_t)f + s - 1, s)), kWave - 1);
     }
-    const uint32_t first = (uint32_t)(upto - mine) * p.Hkv;
-    const uint64_t here = __ballot(at >= first && at < (uint32_t)upto * p.Hkv);
-    if (here != 0) {
-      const int src = __builtin_ctzll(here);
-      b = uniform(base + src);
-      nf = __builtin_amdgcn_readlane(mine, src);
-      ustart = (uint32_t)__builtin_amdgcn_readlane((int)first, src);
-      break;
-    }
-    before = __builtin_amdgcn_readlane(upto, kWave - 1);
+    return n * (uint32_t)p.Hkv;
+  };
+  const bool aligned = share < kFp4LongShare;
+  if (aligned) {
+    // parts a little larger than an equal share, so that all are at work at once; else what is sure to fit, or
+    // (more units than that) whole units in as many turns as it takes
+    int tries = units > room ? 4 : 0;
+    while (tries < 4 && by_units(share) > room) { share += share / 8 + 1; ++tries; }
+    if (tries == 4) share = max(share, units < room ? (total + room - units - 1) / (room - units) : (uint32_t)longest);
   }
-  int h = (int)((at - ustart) / (uint32_t)nf);
-  ustart += (uint32_t)h * (uint32_t)nf;
+  uint32_t at, end, ustart = 0;     // this workgroup's fragments; the first of its unit
+  int b = 0, h, nf = 0, parts_of_unit = 0;
+  uint32_t first_part = 0;          // aligned: the unit's first workgroup
+  {
+    const uint32_t key = aligned ? blockIdx.x : blockIdx.x * share;       // workgroups, or fragments, are numbered through
+    uint32_t from = 0;
+    if (!aligned && key >= total) return;
+    bool found = false;
+    uint32_t frags_before = 0;
+    for (int base = 0; base < p.B; base += kWave) {
+      if (p.B > kWave) mine = base + lane < p.B ? fp4_frags<S, kSparse>(p, base + lane) : 0;
+      const int items = aligned ? (int)small_quotient((uint32_t)mine + share - 1, share) : mine;
+      const int upto_items = wave_inclusive_sum(items);
+      const uint32_t first = from + (uint32_t)(upto_items - items) * p.Hkv, last = from + (uint32_t)upto_items * p.Hkv;
+      const uint64_t here = __ballot(key >= first && key < last);
+      upto = wave_inclusive_sum(mine);
+      if (here != 0) {
+        const int src = __builtin_ctzll(here);
+        b = uniform(base + src);
+        nf = __builtin_amdgcn_readlane(mine, src);
+        first_part = (uint32_t)__builtin_amdgcn_readlane((int)first, src);
+        parts_of_unit = __builtin_amdgcn_readlane(items, src);
+        ustart = frags_before + (uint32_t)__builtin_amdgcn_readlane(upto - mine, src) * (uint32_t)p.Hkv;
+        found = true;
+        break;
+      }
+      from += (uint32_t)__builtin_amdgcn_readlane(upto_items, kWave - 1) * (uint32_t)p.Hkv;
+      frags_before += (uint32_t)__builtin_amdgcn_readlane(upto, kWave - 1) * (uint32_t)p.Hkv;
+    }
+    if (!found) return;
+    h = (int)(aligned ? small_quotient(key - first_part, (uint32_t)parts_of_unit) : (key - first_part) / (uint32_t)parts_of_unit);
+    ustart += (uint32_t)h * (uint32_t)nf;
+    first_part += (uint32_t)h * (uint32_t)parts_of_unit;
+    if (aligned) {
+      const uint32_t chunk = small_quotient((uint32_t)(nf + parts_of_unit) - 1u, (uint32_t)parts_of_unit);
+      at = ustart + (key - first_part) * chunk;
+      end = min(ustart + (uint32_t)nf, at + chunk);
+    } else {
+      at = key;
+      end = min(total, at + share);
+    }
+  }
 
   while (at < end) {
     const int f0 = (int)(at - ustart), f1 = (int)min((uint32_t)nf, end - ustart);
@@ -444,9 +493,12 @@ void fp4_attention_kernel(Fp4Params p) {
     }
     __syncthreads();
     const uint32_t uend = ustart + (uint32_t)nf;
-    const uint32_t w0 = ustart / share, w1 = (uend - 1) / share;
-    const bool whole = w0 == w1;
-    float* mine = p.part + ((size_t)blockIdx.x * 2 + (at > ustart ? 0 : 1)) * p.G * (D + 2);
+    const uint32_t w0 = aligned ? first_part : ustart / share;      // the unit's workgroups
+    const int parts = aligned ? parts_of_unit : (int)((uend - 1) / share - w0) + 1;
+    const bool whole = parts == 1;
+    // (one that reaches into two units it shares with others has a place for either)
+    auto place = [&](uint32_t w) { return p.part + ((size_t)w * 2 + (aligned || w * share > ustart ? 0 : 1)) * p.G * (D + 2); };
+    float* my_part = place(blockIdx.x);
     for (int i = tid; i < p.G * D; i += kFp4Threads) {
       const int g = i / D, c = i % D;
       constexpr int kHalves = kNarrow ? 2 : 1;       // columns of a head
@@ -468,10 +520,10 @@ void fp4_attention_kernel(Fp4Params p) {
         store_fp4_out(p, at_head * D + c, sum > 0.f ? o / sum : 0.f);
         if (p.lse && c == 0) p.lse[at_head] = sum > 0.f ? (M + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
       } else {
-        store_agent(mine + g * (D + 2) + c, o);
+        store_agent(my_part + g * (D + 2) + c, o);
         if (c == 0) {
-          store_agent(mine + g * (D + 2) + D, M);
-          store_agent(mine + g * (D + 2) + D + 1, sum);
+          store_agent(my_part + g * (D + 2) + D, M);
+          store_agent(my_part + g * (D + 2) + D + 1, sum);
         }
       }
     }
@@ -480,17 +532,13 @@ void fp4_attention_kernel(Fp4Params p) {
       __syncthreads();
       if (tid == 0) {
         const int before = atomic_add_agent(p.done + u, 1);
-        last_one = before == (int)(w1 - w0);
+        last_one = before == parts - 1;
         if (last_one) atomic_store_agent(p.done + u, 0);
       }
       __syncthreads();
       if (uniform(last_one)) {
         // maxima and sums of all parts into LDS, their weights over the common maximum from there
-        const int parts = (int)(w1 - w0) + 1;
-        auto part_of = [&](int e) {
-          const uint32_t w = w0 + (uint32_t)e;
-          return p.part + ((size_t)w * 2 + (w * share > ustart ? 0 : 1)) * p.G * (D + 2);
-        };
+        auto part_of = [&](int e) { return place(w0 + (uint32_t)e); };
         float* tops = merge;                        // [parts][G]
         float* sums = merge + parts * p.G;          // [parts][G]
         constexpr int kAhead = 8;                   // parts asked for together
@@ -529,6 +577,7 @@ void fp4_attention_kernel(Fp4Params p) {
       }
     }
     // the next unit
+    if (aligned) return;
     at = uend;
     ustart = uend;
     if (++h == p.Hkv) {

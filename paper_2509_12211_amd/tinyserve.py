@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -114,8 +115,9 @@ def lib():
         L.ts_workspace_bytes.restype = sz
         L.ts_workspace_init.argtypes = [vp, sz, vp]
         L.ts_workspace_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32)]
-        L.ts_rotate_rows.argtypes = [ctypes.POINTER(TsRotary), ctypes.POINTER(TsRows), i32, i32, i32, vp]
-        L.ts_append_rows.argtypes = [lp, ctypes.POINTER(TsRotary), ctypes.POINTER(TsRows), vp, i32, vp]
+        rows = ctypes.c_char_p      # (a packed TsRows)
+        L.ts_rotate_rows.argtypes = [ctypes.POINTER(TsRotary), rows, i32, i32, i32, vp]
+        L.ts_append_rows.argtypes = [lp, ctypes.POINTER(TsRotary), rows, vp, i32, vp]
         L.ts_set_tuning.argtypes = [i32, i32, i32]
         L.ts_debug_xcc_ids.argtypes = [vp, i32, vp]
         L.ts_strerror.argtypes = [ctypes.c_int]
@@ -220,20 +222,22 @@ def make_rotary(cos_sin=None, positions=None, interleaved=False, axis_of_pair=No
     return r
 
 
-def _row_stride(t, like, where):
-    """Elements between the tokens of [num_tokens][heads][d]; like: a tensor of the same tokens and type."""
-    if (t.dim() != 3 or t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] > 1)
-            or t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.shape[2] != like.shape[2]):
+# (The calls of a decode step: a struct packed by format takes a third of what one of ctypes' own does.)
+_pack_rows = struct.Struct("=ii5Q5q").pack
+_ROW_FORMATS = {torch.bfloat16: TS_KV_BF16, torch.float16: TS_KV_FP16}
+
+
+def _row_stride(t, shape, dtype, where):
+    """Elements between the tokens of rows [num_tokens][heads][d], which shape and dtype they must have."""
+    s = t.stride()
+    if t.shape != shape or t.dtype != dtype or s[2] != 1 or (s[1] != shape[2] and shape[1] > 1):
         raise TinyServeError(TS_ERR_SHAPE, where)
-    return t.stride(0)
+    return s[0]
 
 
 def _check_rotary(rotary, tokens, d, where):
-    if (rotary.tokens is not None and rotary.tokens != tokens) or not rotary.norm_dim <= {d}:
+    if (rotary.tokens is not None and rotary.tokens != tokens) or (rotary.norm_dim and rotary.norm_dim != {d}):
         raise TinyServeError(TS_ERR_SHAPE, where)
-
-
-_ROW_FORMATS = {torch.bfloat16: TS_KV_BF16, torch.float16: TS_KV_FP16}
 
 
 def rotate_rows(rotary, q, k, q_out=None, k_out=None):
@@ -241,21 +245,32 @@ def rotate_rows(rotary, q, k, q_out=None, k_out=None):
     None), which may be slices of one projection's rows; in place where no output is given."""
     where = "ts_rotate_rows"
     one = q if q is not None else k
-    if one is None or one.dtype not in _ROW_FORMATS:
+    dtype = None if one is None else one.dtype
+    if dtype not in _ROW_FORMATS:
         raise TinyServeError(TS_ERR_NULL if one is None else TS_ERR_UNSUPPORTED, where)
-    q_out = q if q_out is None else q_out
-    k_out = k if k_out is None else k_out
-    n, _, d = one.shape
-    _check_rotary(rotary, n, d, where)
-    Hq = Hkv = qs = ks = qos = kos = 0
-    if q is not None:
-        Hq, qs, qos = q.shape[1], _row_stride(q, one, where), _row_stride(q_out, one, where)
-    if k is not None:
-        Hkv, ks, kos = k.shape[1], _row_stride(k, one, where), _row_stride(k_out, one, where)
-    if (Hq and q_out.shape[1] != Hq) or (Hkv and k_out.shape[1] != Hkv):
+    shape = one.shape
+    if len(shape) != 3:
         raise TinyServeError(TS_ERR_SHAPE, where)
-    rows = TsRows(n, _ROW_FORMATS[one.dtype], _ptr(q), _ptr(k), None, _ptr(q_out), _ptr(k_out), qs, ks, 0, qos, kos)
-    _check(lib().ts_rotate_rows(ctypes.byref(rotary), ctypes.byref(rows), Hq, Hkv, d, _stream()), where)
+    n, _, d = shape
+    _check_rotary(rotary, n, d, where)
+    Hq = Hkv = qs = ks = qos = kos = qp = kp = qop = kop = 0
+    if q is not None:
+        Hq, qp = shape[1], q.data_ptr()
+        qs = qos = _row_stride(q, shape, dtype, where)
+        qop = qp
+        if q_out is not None:
+            qos, qop = _row_stride(q_out, shape, dtype, where), q_out.data_ptr()
+    if k is not None:
+        shape = k.shape
+        if len(shape) != 3 or shape[0] != n or shape[2] != d:
+            raise TinyServeError(TS_ERR_SHAPE, where)
+        Hkv, kp = shape[1], k.data_ptr()
+        ks = kos = _row_stride(k, shape, dtype, where)
+        kop = kp
+        if k_out is not None:
+            kos, kop = _row_stride(k_out, shape, dtype, where), k_out.data_ptr()
+    rows = _pack_rows(n, _ROW_FORMATS[dtype], qp, kp, 0, qop, kop, qs, ks, 0, qos, kos)
+    _check(lib().ts_rotate_rows(ctypes.byref(rotary), rows, Hq, Hkv, d, _stream()), where)
 
 
 def append_rows(layout, k, v, rotary=None, q=None, q_out=None, cu_tokens=None, advance_seq_lens=True,
@@ -265,27 +280,30 @@ def append_rows(layout, k, v, rotary=None, q=None, q_out=None, cu_tokens=None, a
     [num_tokens][Hq][d] is normed and rotated into q_out (in place if none is given) in the same
     launch.  lens_include_new: the layout's lengths count the new tokens already."""
     where = "ts_append_rows"
-    half = layout.kv_format == TS_KV_FP16
-    if k.dtype != (torch.float16 if half else torch.bfloat16):
+    dtype, shape = k.dtype, k.shape
+    if dtype != (torch.float16 if layout.kv_format == TS_KV_FP16 else torch.bfloat16):
         raise TinyServeError(TS_ERR_UNSUPPORTED, where)
-    n, Hkv, d = k.shape
+    if len(shape) != 3 or shape[1] != layout.num_kv_heads or shape[2] != layout.head_dim or (
+            shape[0] != layout.num_seqs if cu_tokens is None else
+            cu_tokens.dtype != torch.int32 or cu_tokens.numel() != layout.num_seqs + 1 or not cu_tokens.is_contiguous()):
+        raise TinyServeError(TS_ERR_SHAPE, where)
+    n, _, d = shape
+    ref = None
     if rotary is not None:
         _check_rotary(rotary, n, d, where)
-    qs = qos = 0
+        ref = ctypes.byref(rotary)
+    ks, vs = _row_stride(k, shape, dtype, where), _row_stride(v, shape, dtype, where)
+    qs = qos = qp = qop = 0
     if q is not None:
-        q_out = q if q_out is None else q_out
-        qs, qos = _row_stride(q, k, where), _row_stride(q_out, k, where)
-        if q.shape[1] != layout.num_q_heads or q_out.shape[1] != layout.num_q_heads:
-            raise TinyServeError(TS_ERR_SHAPE, where)
-    ks, vs = _row_stride(k, k, where), _row_stride(v, k, where)
-    if Hkv != layout.num_kv_heads or v.shape[1] != Hkv or d != layout.head_dim or (
-            n != layout.num_seqs if cu_tokens is None else
-            cu_tokens.dtype != torch.int32 or cu_tokens.numel() != layout.num_seqs + 1):
-        raise TinyServeError(TS_ERR_SHAPE, where)
+        shape = (n, layout.num_q_heads, d)
+        qp = qop = q.data_ptr()
+        qs = qos = _row_stride(q, shape, dtype, where)
+        if q_out is not None:
+            qos, qop = _row_stride(q_out, shape, dtype, where), q_out.data_ptr()
     lens = TS_LENS_AFTER if lens_include_new else TS_LENS_ADVANCE if advance_seq_lens else TS_LENS_KEEP
-    rows = TsRows(n, 0, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out) if q is not None else None, None, qs, ks, vs, qos, 0)
-    _check(lib().ts_append_rows(ctypes.byref(layout), None if rotary is None else ctypes.byref(rotary),
-                                ctypes.byref(rows), _ptr(cu_tokens), lens, _stream()), where)
+    rows = _pack_rows(n, 0, qp, k.data_ptr(), v.data_ptr(), qop, 0, qs, ks, vs, qos, 0)
+    _check(lib().ts_append_rows(ctypes.byref(layout), ref, rows, None if cu_tokens is None else cu_tokens.data_ptr(),
+                                lens, _stream()), where)
 
 
 def build_page_meta(layout):

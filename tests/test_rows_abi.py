@@ -45,13 +45,13 @@ def fp4(**kw):
 
 
 def rotate(r, w, Hq=8, Hkv=2, d=64):
-    return ts.lib().ts_rotate_rows(None if r is None else ctypes.byref(r), None if w is None else ctypes.byref(w), Hq,
-                                   Hkv, d, None)
+    return ts.lib().ts_rotate_rows(None if r is None else ctypes.byref(r), None if w is None else bytes(w), Hq, Hkv, d,
+                                   None)
 
 
 def append(lay, r, w, cu=P, lens=0):
     return ts.lib().ts_append_rows(None if lay is None else ctypes.byref(lay), None if r is None else ctypes.byref(r),
-                                   None if w is None else ctypes.byref(w), cu, lens, None)
+                                   None if w is None else bytes(w), cu, lens, None)
 
 
 @pytest.mark.parametrize("struct,mirror", [("ts_rotary", ts.TsRotary), ("ts_rows", ts.TsRows)])
@@ -65,6 +65,11 @@ def test_struct_layouts_match_the_header(tmp_path, struct, mirror):
     subprocess.run(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
     got = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
     assert got == [ctypes.sizeof(mirror)] + [getattr(mirror, n).offset for n in fields]
+
+
+def test_the_packed_rows_are_the_struct():
+    values = list(range(3, 15))
+    assert ts._pack_rows(*values) == bytes(ts.TsRows(*values))
 
 
 BAD_ROTARY = [
