@@ -537,38 +537,33 @@ void fp4_attention_kernel(Fp4Params p) {
       }
       __syncthreads();
       if (uniform(last_one)) {
-        // maxima and sums of all parts into LDS, their weights over the common maximum from there
-        auto part_of = [&](int e) { return place(w0 + (uint32_t)e); };
-        float* tops = merge;                        // [parts][G]
-        float* sums = merge + parts * p.G;          // [parts][G]
-        constexpr int kAhead = 8;                   // parts asked for together
-        float x[kAhead];
-        auto fetch = [&](int i, int e0) {
-#pragma unroll
-          for (int e = 0; e < kAhead; ++e) x[e] = load_agent(part_of(min(e0 + e, parts - 1)) + i / D * (D + 2) + i % D);
-        };
-        if (tid < p.G * D) fetch(tid, 0);
-        for (int i = tid; i < parts * p.G; i += kFp4Threads) {
-          const float* row = part_of(i / p.G) + (i % p.G) * (D + 2) + D;
-          tops[i] = load_agent(row);
-          sums[i] = load_agent(row + 1);
-        }
-        __syncthreads();
+        // (a part's maximum, sum and number asked for together, eight parts at a time)
         for (int i = tid; i < p.G * D; i += kFp4Threads) {
           const int g = i / D, c = i % D;
+          constexpr int kAhead = 8;
           float M = -INFINITY, o = 0.f, sum = 0.f;
-          for (int e = 0; e < parts; ++e) M = fmaxf(M, tops[e * p.G + g]);
-          const float ref = M == -INFINITY ? 0.f : M;
           for (int e0 = 0; e0 < parts; e0 += kAhead) {
-            if (e0 != 0 || i != tid) fetch(i, e0);
+            float m[kAhead], x[kAhead], z[kAhead];
 #pragma unroll
             for (int e = 0; e < kAhead; ++e) {
-              if (e0 + e < parts) {
-                const float a = __builtin_amdgcn_exp2f(tops[(e0 + e) * p.G + g] - ref);
-                o += x[e] * a;
-                sum += sums[(e0 + e) * p.G + g] * a;
-              }
+              const float* part = place(w0 + (uint32_t)min(e0 + e, parts - 1)) + g * (D + 2);
+              m[e] = load_agent(part + D);
+              x[e] = load_agent(part + c);
+              z[e] = load_agent(part + D + 1);
             }
+            float top = M;
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) top = raw_max(top, m[e]);
+            const float ref = top == -INFINITY ? 0.f : top, a = __builtin_amdgcn_exp2f(M - ref);
+            o *= a;
+            sum *= a;
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+              const float k = e0 + e < parts ? __builtin_amdgcn_exp2f(m[e] - ref) : 0.f;
+              o += x[e] * k;
+              sum += z[e] * k;
+            }
+            M = top;
           }
           const size_t at_head = (size_t)b * p.Hq + h * p.G + g;
           store_fp4_out(p, at_head * D + c, sum > 0.f ? o / sum : 0.f);
