@@ -133,7 +133,8 @@ typedef struct ts_layout {
    * to 7, the sign in bit 3), one positive bf16 scale per token, KV head, and key or
    * value; the number is code * scale.  k_pool points to one block of
    * page_size * (d + 4) bytes per (physical page, head), kv_tile_stride bytes apart
-   * (0: dense; a multiple of 16); v_pool, k_scale and v_scale are not looked at.
+   * (0: dense; a multiple of 16), 16-byte aligned; v_pool, k_scale and v_scale are
+   * not looked at.
    * A block holds, in this order,
    *   keys    [S][d/2]              two channels a byte, the even one in the low half
    *   values  [S/8][d/64][16][4][4] four bytes are the eight tokens 8o .. 8o+7 of one

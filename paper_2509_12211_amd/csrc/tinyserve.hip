@@ -304,6 +304,8 @@ static int check_layout(const ts_layout* L) {
   return TS_OK;
 }
 
+static bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
 // The pool pointers every call that attends (or appends into the pool) needs:
 // K and V tiles, the block table, the lengths and, for the INT8 cache, the two
 // per-token scale arrays the kernels dereference.
@@ -311,6 +313,7 @@ static int check_pool(const ts_layout* L) {
   if (!L->k_pool || !L->block_table || !L->seq_lens) return TS_ERR_NULL;
   if (L->kv_format != TS_KV_FP4 && !L->v_pool) return TS_ERR_NULL;   // (4 bits: one block holds both)
   if (L->kv_format == TS_KV_INT8 && (!L->k_scale || !L->v_scale)) return TS_ERR_NULL;
+  if (L->kv_format == TS_KV_FP4 && !aligned(L->k_pool, 16)) return TS_ERR_SHAPE;
   return TS_OK;
 }
 
@@ -395,7 +398,8 @@ static Fp4Plan make_fp4_plan(const ts_layout* L, int pages, bool query_aware) {
   pl.workgroups = pl.room > units ? pl.room : units;
   size_t off = kCtrlArea * sizeof(int32_t);
   pl.off_done = off;
-  off = align_up(off + (size_t)units * sizeof(int32_t), 256);
+  // (the counts lie at the same place whatever the batch, so that batches of several shapes can take turns)
+  off = align_up(off + (size_t)kFp4Counters * sizeof(int32_t), 256);
   pl.off_part = off;
   off = align_up(off + (size_t)pl.room * 2 * G * (L->head_dim + 2) * sizeof(float), 256);
   pl.attend_total = off;
@@ -478,8 +482,6 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
 // ---------------------------------------------------------------------------
 // Rows of queries and keys
 // ---------------------------------------------------------------------------
-static bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-
 static int check_rotary(const ts_rotary* r, int head_dim, bool needs_positions) {
   if (r->rot_dim < 0 || r->rot_dim > head_dim || r->rot_dim % 8 != 0) return TS_ERR_SHAPE;
   if (!aligned(r->q_norm, 16) || !aligned(r->k_norm, 16) || !(r->norm_eps >= 0.f)) return TS_ERR_SHAPE;
@@ -761,6 +763,7 @@ int ts_build_page_meta(const ts_layout* layout, void* stream) {
   MetaParams p = meta_params(layout);
   if (p.B > 65535) return TS_ERR_UNSUPPORTED;
   const bool int8 = layout->kv_format == TS_KV_INT8, fp4 = layout->kv_format == TS_KV_FP4;
+  if (fp4 && !aligned(layout->k_pool, 16)) return TS_ERR_SHAPE;
   if (int8 && !layout->k_scale) return TS_ERR_NULL;
   const int pages_per_wg = kWaves * (int8 ? 8 : kWave / (layout->head_dim / (fp4 ? 32 : 8)));
   // (the KV head is the fastest grid index: a physical page's tiles of all heads are
@@ -817,6 +820,7 @@ int ts_append_token_meta(const ts_layout* layout, const void* k_new, const void*
   if (!k_new || !layout->seq_lens || !layout->page_min || !layout->page_max) return TS_ERR_NULL;
   if (layout->kv_format == TS_KV_FP4) {
     if (!layout->block_table || (v_new && !layout->k_pool)) return TS_ERR_NULL;
+    if (!aligned(layout->k_pool, 16)) return TS_ERR_SHAPE;
     return append_fp4_token(layout, k_new, v_new, advance_seq_lens, (hipStream_t)stream);
   }
   if (v_new && (!layout->k_pool || !layout->v_pool || !layout->block_table)) return TS_ERR_NULL;

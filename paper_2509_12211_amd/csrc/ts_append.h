@@ -409,7 +409,7 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
   for (int i = 0; i < 8; ++i) { lo[i] = INFINITY; hi[i] = -INFINITY; }
   for (int i0 = group % tp; i0 < ntok; i0 += tp) {
     const int tok = tok0 + i0, slot = slot0 + i0;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 2;
     const uint16_t* q_src = p.q + tok * p.q_stride + (size_t)h * p.G * D;
     uint2 qa[kAhead], qb[kAhead], ka, kb, va, vb;
     // (the number of rounds is the same for all: a group without a row in the last one fetches another's)

@@ -26,6 +26,7 @@ namespace ts {
 constexpr int kFp4Frag = 32;            // tokens of a fragment
 constexpr int kFp4List = 1024;          // list entries held in LDS at a time
 constexpr int kFp4Parts = 64;           // about how many workgroups share a unit at the most
+constexpr int kFp4Counters = 1024;      // places for counts, whatever the batch
 constexpr uint32_t kFp4LongShare = 192; // fragments of a workgroup from which on all get the same number
 
 // Workgroups of eight waves, two on a compute unit, for 64 channels; with 128, where a wave's registers leave
@@ -37,6 +38,7 @@ struct Fp4Shape {
   static constexpr int kPerCu = D == 64 ? 2 : 3;              // workgroups on a compute unit
   static constexpr int kStages = D == 64 ? 3 : 2;             // fragments a wave has room for
   static constexpr int kResident = 256 * kPerCu;
+  static_assert(kResident <= kFp4Counters, "a count for each");
   static constexpr int kMinShare = 16;                        // fragments a workgroup has at the least
   // a fragment in LDS: keys, values, scales
   static constexpr int kKeys = 0, kValues = 16 * D, kScales = 32 * D, kStage = 32 * D + 256;
@@ -56,7 +58,7 @@ struct Fp4Params {
   float* out;                       // [B][Hq][D] fp32 or bf16
   float* lse;                       // nullable [B][Hq]
   float* part;                      // [room][2][G][D + 2]: what a unit's workgroups hand over
-  int32_t* done;                    // [units] workgroups that have; zero between launches
+  int32_t* done;                    // [room] by a shared unit's first workgroup: how many have; zero between launches
   int B, Hq, Hkv, G, Pmax, Kmax, n_phys, out_bf16;
   int room;                         // workgroups that have a place in part, and are at work at once
   long long tile_stride;
@@ -505,20 +507,20 @@ void fp4_attention_kernel(Fp4Params p) {
       float M = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kFp4Waves * kHalves; ++w) M = fmaxf(M, merge[w / kHalves * kWaveRows + (g + w % kHalves * 8) * kRow + D]);
+      // (a wave without a token has zeros and the weight 0; what is not a number stays so)
+      const float ref = M == -INFINITY ? 0.f : M;
       float o = 0.f, sum = 0.f;
-      if (M != -INFINITY) {
 #pragma unroll
-        for (int w = 0; w < kFp4Waves * kHalves; ++w) {
-          const float* row = merge + w / kHalves * kWaveRows + (g + w % kHalves * 8) * kRow;
-          const float a = __builtin_amdgcn_exp2f(row[D] - M);
-          o += a * row[c];
-          sum += a * row[D + 1];
-        }
+      for (int w = 0; w < kFp4Waves * kHalves; ++w) {
+        const float* row = merge + w / kHalves * kWaveRows + (g + w % kHalves * 8) * kRow;
+        const float a = __builtin_amdgcn_exp2f(row[D] - ref);
+        o += a * row[c];
+        sum += a * row[D + 1];
       }
       if (whole) {
         const size_t at_head = (size_t)b * p.Hq + h * p.G + g;
-        store_fp4_out(p, at_head * D + c, sum > 0.f ? o / sum : 0.f);
-        if (p.lse && c == 0) p.lse[at_head] = sum > 0.f ? (M + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        store_fp4_out(p, at_head * D + c, sum == 0.f ? 0.f : o / sum);
+        if (p.lse && c == 0) p.lse[at_head] = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * 0.6931471805599453f;
       } else {
         store_agent(my_part + g * (D + 2) + c, o);
         if (c == 0) {
@@ -531,9 +533,9 @@ void fp4_attention_kernel(Fp4Params p) {
       stores_complete();
       __syncthreads();
       if (tid == 0) {
-        const int before = atomic_add_agent(p.done + u, 1);
+        const int before = atomic_add_agent(p.done + w0, 1);
         last_one = before == parts - 1;
-        if (last_one) atomic_store_agent(p.done + u, 0);
+        if (last_one) atomic_store_agent(p.done + w0, 0);
       }
       __syncthreads();
       if (uniform(last_one)) {
@@ -566,8 +568,8 @@ void fp4_attention_kernel(Fp4Params p) {
             M = top;
           }
           const size_t at_head = (size_t)b * p.Hq + h * p.G + g;
-          store_fp4_out(p, at_head * D + c, sum > 0.f ? o / sum : 0.f);
-          if (p.lse && c == 0) p.lse[at_head] = sum > 0.f ? (M + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
+          store_fp4_out(p, at_head * D + c, sum == 0.f ? 0.f : o / sum);
+          if (p.lse && c == 0) p.lse[at_head] = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * 0.6931471805599453f;
         }
       }
     }

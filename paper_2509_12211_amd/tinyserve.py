@@ -143,6 +143,13 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _stream_on(device, where):
+    """The current stream, of the device that the tensors are on."""
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise TinyServeError(TS_ERR_DEVICE, where)
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _check(status, where):
     if status != TS_OK:
         raise TinyServeError(status, where)
@@ -206,10 +213,14 @@ def make_rotary(cos_sin=None, positions=None, interleaved=False, axis_of_pair=No
     The tensors are held by the struct."""
     axes = 1 if positions is None or positions.dim() == 1 else positions.shape[0]
     rows, rot = (0, 0) if cos_sin is None else cos_sin.shape
-    for t, dtype in ((cos_sin, torch.float32), (positions, torch.int32), (q_norm, torch.float32),
-                     (k_norm, torch.float32)):
-        if t is not None and (t.dtype != dtype or not t.is_contiguous()):
+    held = [(t, dtype) for t, dtype in ((cos_sin, torch.float32), (positions, torch.int32), (q_norm, torch.float32),
+                                        (k_norm, torch.float32)) if t is not None]
+    for t, dtype in held:
+        if t.dtype != dtype or not t.is_contiguous():
             raise TinyServeError(TS_ERR_SHAPE, "make_rotary")
+    devices = {t.get_device() for t, _ in held}
+    if len(devices) > 1:
+        raise TinyServeError(TS_ERR_DEVICE, "make_rotary")
     r = TsRotary(rot, int(interleaved), axes, rows, _ptr(cos_sin), _ptr(positions), _ptr(q_norm), _ptr(k_norm),
                  float(norm_eps))
     if axes > 1:
@@ -218,6 +229,7 @@ def make_rotary(cos_sin=None, positions=None, interleaved=False, axis_of_pair=No
         r.axis_of_pair[:rot // 2] = [int(a) for a in axis_of_pair]
     r.held = (cos_sin, positions, q_norm, k_norm)
     r.tokens = None if positions is None else positions.shape[-1]
+    r.device = devices.pop() if devices else None
     r.norm_dim = {t.numel() for t in (q_norm, k_norm) if t is not None}
     return r
 
@@ -227,15 +239,19 @@ _pack_rows = struct.Struct("=ii5Q5q").pack
 _ROW_FORMATS = {torch.bfloat16: TS_KV_BF16, torch.float16: TS_KV_FP16}
 
 
-def _row_stride(t, shape, dtype, where):
-    """Elements between the tokens of rows [num_tokens][heads][d], which shape and dtype they must have."""
+def _row_stride(t, shape, dtype, device, where):
+    """Elements between the tokens of rows [num_tokens][heads][d], which shape, dtype and device they must have."""
     s = t.stride()
+    if t.get_device() != device:
+        raise TinyServeError(TS_ERR_DEVICE, where)
     if t.shape != shape or t.dtype != dtype or s[2] != 1 or (s[1] != shape[2] and shape[1] > 1):
         raise TinyServeError(TS_ERR_SHAPE, where)
     return s[0]
 
 
-def _check_rotary(rotary, tokens, d, where):
+def _check_rotary(rotary, tokens, d, device, where):
+    if rotary.device is not None and rotary.device != device:
+        raise TinyServeError(TS_ERR_DEVICE, where)
     if (rotary.tokens is not None and rotary.tokens != tokens) or (rotary.norm_dim and rotary.norm_dim != {d}):
         raise TinyServeError(TS_ERR_SHAPE, where)
 
@@ -252,25 +268,26 @@ def rotate_rows(rotary, q, k, q_out=None, k_out=None):
     if len(shape) != 3:
         raise TinyServeError(TS_ERR_SHAPE, where)
     n, _, d = shape
-    _check_rotary(rotary, n, d, where)
+    device = one.get_device()
+    _check_rotary(rotary, n, d, device, where)
     Hq = Hkv = qs = ks = qos = kos = qp = kp = qop = kop = 0
     if q is not None:
         Hq, qp = shape[1], q.data_ptr()
-        qs = qos = _row_stride(q, shape, dtype, where)
+        qs = qos = _row_stride(q, shape, dtype, device, where)
         qop = qp
         if q_out is not None:
-            qos, qop = _row_stride(q_out, shape, dtype, where), q_out.data_ptr()
+            qos, qop = _row_stride(q_out, shape, dtype, device, where), q_out.data_ptr()
     if k is not None:
         shape = k.shape
         if len(shape) != 3 or shape[0] != n or shape[2] != d:
             raise TinyServeError(TS_ERR_SHAPE, where)
         Hkv, kp = shape[1], k.data_ptr()
-        ks = kos = _row_stride(k, shape, dtype, where)
+        ks = kos = _row_stride(k, shape, dtype, device, where)
         kop = kp
         if k_out is not None:
-            kos, kop = _row_stride(k_out, shape, dtype, where), k_out.data_ptr()
+            kos, kop = _row_stride(k_out, shape, dtype, device, where), k_out.data_ptr()
     rows = _pack_rows(n, _ROW_FORMATS[dtype], qp, kp, 0, qop, kop, qs, ks, 0, qos, kos)
-    _check(lib().ts_rotate_rows(ctypes.byref(rotary), rows, Hq, Hkv, d, _stream()), where)
+    _check(lib().ts_rotate_rows(ctypes.byref(rotary), rows, Hq, Hkv, d, _stream_on(device, where)), where)
 
 
 def append_rows(layout, k, v, rotary=None, q=None, q_out=None, cu_tokens=None, advance_seq_lens=True,
@@ -285,25 +302,25 @@ def append_rows(layout, k, v, rotary=None, q=None, q_out=None, cu_tokens=None, a
         raise TinyServeError(TS_ERR_UNSUPPORTED, where)
     if len(shape) != 3 or shape[1] != layout.num_kv_heads or shape[2] != layout.head_dim or (
             shape[0] != layout.num_seqs if cu_tokens is None else
-            cu_tokens.dtype != torch.int32 or cu_tokens.numel() != layout.num_seqs + 1 or not cu_tokens.is_contiguous()):
+            cu_tokens.get_device() != k.get_device() or cu_tokens.dtype != torch.int32 or cu_tokens.numel() != layout.num_seqs + 1 or not cu_tokens.is_contiguous()):
         raise TinyServeError(TS_ERR_SHAPE, where)
     n, _, d = shape
-    ref = None
+    device, ref = k.get_device(), None
     if rotary is not None:
-        _check_rotary(rotary, n, d, where)
+        _check_rotary(rotary, n, d, device, where)
         ref = ctypes.byref(rotary)
-    ks, vs = _row_stride(k, shape, dtype, where), _row_stride(v, shape, dtype, where)
+    ks, vs = _row_stride(k, shape, dtype, device, where), _row_stride(v, shape, dtype, device, where)
     qs = qos = qp = qop = 0
     if q is not None:
         shape = (n, layout.num_q_heads, d)
         qp = qop = q.data_ptr()
-        qs = qos = _row_stride(q, shape, dtype, where)
+        qs = qos = _row_stride(q, shape, dtype, device, where)
         if q_out is not None:
-            qos, qop = _row_stride(q_out, shape, dtype, where), q_out.data_ptr()
+            qos, qop = _row_stride(q_out, shape, dtype, device, where), q_out.data_ptr()
     lens = TS_LENS_AFTER if lens_include_new else TS_LENS_ADVANCE if advance_seq_lens else TS_LENS_KEEP
     rows = _pack_rows(n, 0, qp, k.data_ptr(), v.data_ptr(), qop, 0, qs, ks, vs, qos, 0)
     _check(lib().ts_append_rows(ctypes.byref(layout), ref, rows, None if cu_tokens is None else cu_tokens.data_ptr(),
-                                lens, _stream()), where)
+                                lens, _stream_on(device, where)), where)
 
 
 def build_page_meta(layout):

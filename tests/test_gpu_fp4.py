@@ -305,6 +305,50 @@ def test_long_sequences_shared_by_many_workgroups():
         c.check(c.out, c.lse, scale, what="long")
 
 
+def test_batches_of_several_shapes_take_turns_on_one_workspace():
+    """Counts and partial results of one batch never stand where another's counts do."""
+    g = torch.Generator().manual_seed(8)
+    batches = [Fp4([9000, 40], 8, 2, 64, 16, g), Fp4([700] * 40, 4, 4, 128, 32, g), Fp4([30] * 300, 2, 2, 64, 8, g),
+               Fp4([20000], 16, 1, 128, 64, g)]
+    size = max(ts.new_dense_workspace(c.layout, DEV).numel() for c in batches)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    ts.workspace_init(ws)
+    for rnd in range(2):
+        for c in batches + batches[::-1]:
+            c.out.fill_(math.nan)
+            ts.dense_decode_attention(c.layout, c.q, 0.125, c.out, ws, lse_out=c.lse)
+            if rnd == 0:
+                c.first = c.out.clone()
+            assert torch.equal(c.first, c.out)
+    for c in batches:
+        c.check(c.out, c.lse, 0.125, what="turns")
+
+
+@pytest.mark.parametrize("B,lens,Hq,Hkv,d", [(70, (1, 90), 4, 2, 64), (100, (1, 2500), 16, 8, 128), (130, (0, 40), 32, 8, 64),
+                                             (3, (6000, 9000), 64, 64, 64)])
+def test_many_units(B, lens, Hq, Hkv, d):
+    """More sequences than a wave has lanes, more units than workgroups at once, whole units and shares."""
+    g = torch.Generator().manual_seed(B)
+    n = torch.randint(lens[0], lens[1] + 1, (B,), generator=g).tolist()
+    c = Fp4(n, Hq, Hkv, d, 16, g)
+    ws = ts.new_dense_workspace(c.layout, DEV)
+    ts.dense_decode_attention(c.layout, c.q, 0.2, c.out, ws, lse_out=c.lse)
+    c.check(c.out, c.lse, 0.2, what="many")
+
+
+def test_what_is_not_a_number_stays_with_its_head():
+    c = Fp4([3000, 17], 8, 2, 64, 16, torch.Generator().manual_seed(9))
+    ws = ts.new_dense_workspace(c.layout, DEV)
+    clean = torch.empty_like(c.out)
+    ts.dense_decode_attention(c.layout, c.q, 0.125, clean, ws)
+    c.q[0, 5, 3] = math.nan
+    c.q[1, 0, :] = math.nan
+    ts.dense_decode_attention(c.layout, c.q, 0.125, c.out, ws)
+    bad = torch.zeros(c.out.shape[:2], dtype=torch.bool)
+    bad[0, 5] = bad[1, 0] = True
+    assert c.out.cpu()[bad].isnan().all() and torch.equal(c.out.cpu()[~bad], clean.cpu()[~bad])
+
+
 def test_captured_attention_is_replayed():
     c = Fp4([5000, 100, 1], 8, 2, 64, 16, torch.Generator().manual_seed(6))
     scale = 0.125

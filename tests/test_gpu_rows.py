@@ -245,6 +245,34 @@ def test_one_token_each_without_offsets(fmt, S):
                                                             y.nan_to_num(9.0) if y.is_floating_point() else y)
 
 
+@pytest.mark.parametrize("fmt,S", [("bf16", 16), ("int8", 8), ("fp4", 32)])
+def test_lengths_that_count_the_new_tokens_already(fmt, S):
+    """Ragged appends with the lengths before and after give the same cache; positions by several axes."""
+    g = torch.Generator().manual_seed(S)
+    B, Hq, Hkv, d, wide = 3, 2, 1, 64, 5
+    before, after = (Cache(fmt, B, Hkv, d, S, wide, torch.Generator().manual_seed(4), Hq) for _ in range(2))
+    table = ts.rotary_table(40, d, device=DEV)
+    axis = [i % 3 for i in range(d // 2)]
+    outs = {}
+    for counts in ([S + 3, 1, 0], [2, S, 2 * S + 1]):
+        n = sum(counts)
+        q, k, v = rows_of(n, [Hq, Hkv, Hkv], d, before.dtype, g, fused=True)
+        pos = torch.randint(0, 40, (3, n), generator=g, dtype=torch.int32).to(DEV)
+        r = ts.make_rotary(table, positions=pos, interleaved=True, axis_of_pair=axis)
+        cu = torch.tensor([0] + counts).cumsum(0).int().to(DEV)
+        for c in (before, after):
+            if c is after:
+                c.lens += cu[1:] - cu[:-1]
+            outs[c] = torch.empty_like(q)
+            ts.append_rows(c.layout, k, v, rotary=r, q=q, q_out=outs[c], cu_tokens=cu, lens_include_new=c is after)
+        wq = torch.empty_like(q)
+        ts.rotate_rows(r, q, None, wq)
+        assert torch.equal(outs[before], wq) and torch.equal(outs[after], wq)
+        for x, y in zip(before.state(), after.state()):
+            assert (x is None and y is None) or torch.equal(x.nan_to_num(9.0) if x.is_floating_point() else x,
+                                                            y.nan_to_num(9.0) if y.is_floating_point() else y)
+
+
 @pytest.mark.parametrize("fmt,S", FORMATS)
 def test_boxes_and_slots_as_token_by_token(fmt, S):
     """Without rotation: the same cache as ts_append_token_meta leaves, called once for each token."""

@@ -139,6 +139,7 @@ def test_append_refuses_other_arguments():
     (dict(kv_tile_stride=1072), ts.TS_ERR_SHAPE),       # less than a block of 16 * 68 bytes
     (dict(kv_tile_stride=1096), ts.TS_ERR_SHAPE),       # blocks must stay 16-byte aligned
     (dict(head_dim=96), ts.TS_ERR_UNSUPPORTED), (dict(kv_format=4), ts.TS_ERR_UNSUPPORTED),
+    (dict(k_pool=P + 8), ts.TS_ERR_SHAPE),              # and so must their pool
 ])
 def test_four_bit_layouts_out_of_range_are_refused(kw, code):
     lay, L = fp4(**kw), ts.lib()
@@ -147,8 +148,9 @@ def test_four_bit_layouts_out_of_range_are_refused(kw, code):
     assert L.ts_append_token_meta(ref_, P, P, 1, None) == code
     assert L.ts_dense_decode_attention(ref_, P, 1.0, P, None, P, 1 << 30, None) == code
     assert L.ts_query_aware_decode(ref_, P, 4, None, 4, 1.0, P, None, None, None, P, 1 << 30, None) == code
-    assert L.ts_append_and_decode_launches(ref_, 4) == code
-    assert ts.workspace_bytes(lay, 4) == 0
+    if "k_pool" not in kw:      # (these two look at the shape alone)
+        assert L.ts_append_and_decode_launches(ref_, 4) == code
+        assert ts.workspace_bytes(lay, 4) == 0
 
 
 def test_four_bit_calls_check_their_pointers_and_workspaces():
@@ -198,7 +200,9 @@ def test_binding_refuses_tensors_that_do_not_fit():
                  lambda: ts.append_rows(layout(), kv, kv, q=bf[:, :4]),
                  lambda: ts.append_rows(layout(), kv, kv, cu_tokens=torch.zeros(4, dtype=torch.int32)),
                  lambda: ts.append_rows(layout(), kv, kv, cu_tokens=torch.zeros(3)),
-                 lambda: ts.append_rows(layout(), kv, kv)):                            # four tokens, two sequences
+                 lambda: ts.append_rows(layout(), kv, kv),                             # four tokens, two sequences
+                 lambda: ts.append_rows(layout(num_seqs=4), kv, kv),                   # tensors that no GPU can read
+                 lambda: ts.rotate_rows(ts.make_rotary(), bf, kv)):
         with pytest.raises(ts.TinyServeError):
             call()
 
