@@ -587,10 +587,12 @@ void fp4_attention_kernel(Fp4Params p) {
 }
 
 // Rebuild of the boxes: a page's D / 32 lanes own 32 channels each (16 bytes of a token's row) and walk
-// down its tokens.  code * scale is exact in fp32, so the extremes are, and are rounded outwards to bf16.
+// down its tokens, eight rows and their scales asked for together.  code * scale is exact in fp32, so the extremes
+// are, and are rounded outwards to bf16.  Bound by memory.
 template <int D>
 __global__ __launch_bounds__(kThreads) void build_page_meta_fp4_kernel(MetaParams p) {
   constexpr int LPP = D / 32, PPW = kWave / LPP;    // lanes a page, pages a wave
+  constexpr int NT = 8;
   const int lane = lane_id(), cg = lane % LPP;
   const int first = (blockIdx.y * kWaves + wave_id()) * PPW, j = first + lane / LPP;
   const int h = blockIdx.x, b = blockIdx.z;
@@ -599,25 +601,34 @@ __global__ __launch_bounds__(kThreads) void build_page_meta_fp4_kernel(MetaParam
   if (uniform(first) >= Pb) return;
   const int phys = p.block_table[(size_t)b * p.Pmax + min(j, Pb - 1)];
   const bool on = j < Pb && phys >= 0 && phys < p.n_phys;
-  const int tokens = on ? min(p.S, L - j * p.S) : 0;
+  const int tokens = min(p.S, L - j * p.S);   // (only looked at where `on`)
   const unsigned char* tile = reinterpret_cast<const unsigned char*>(p.k_pool) +
                               ((size_t)(on ? phys : 0) * p.Hkv + h) * (size_t)p.tile_stride;
-  const uint16_t* scales = reinterpret_cast<const uint16_t*>(tile + Fp4Block<D>::key_scales(p.S));
+  const unsigned char* scales = tile + Fp4Block<D>::key_scales(p.S);
   float lo[32], hi[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) { lo[i] = INFINITY; hi[i] = -INFINITY; }
-  for (int t = 0; t < tokens; ++t) {
-    const uint4 w4 = *reinterpret_cast<const uint4*>(tile + t * (D / 2) + cg * 16);
-    const float s = bf16_to_f32(scales[t]);
-    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+  for (int t0 = 0; t0 < p.S; t0 += NT) {
+    uint4 w[NT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bf16x8_t v = fp4_operand(w[i]);
+    for (int t = 0; t < NT; ++t) w[t] = *reinterpret_cast<const uint4*>(tile + (t0 + t) * (D / 2) + cg * 16);
+    const uint4 s4 = *reinterpret_cast<const uint4*>(scales + 2 * t0);
+    float s[NT];
+    unpack8(s4, s);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const float x = (float)v[c] * s;
-        lo[8 * i + c] = fminf(lo[8 * i + c], x);
-        hi[8 * i + c] = fmaxf(hi[8 * i + c], x);
+    for (int t = 0; t < NT; ++t) {
+      // (a slot without a token gets a scale that makes no number, which gives way in every comparison)
+      const float scale = t0 + t < tokens ? s[t] : __uint_as_float(0x7fc00000u);
+      const uint32_t x[4] = {w[t].x, w[t].y, w[t].z, w[t].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[8];
+        fp4_numbers(x[i], scale, v);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          lo[8 * i + c] = raw_min(lo[8 * i + c], v[c]);
+          hi[8 * i + c] = raw_max(hi[8 * i + c], v[c]);
+        }
       }
     }
   }
