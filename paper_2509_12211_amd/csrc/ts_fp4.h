@@ -36,7 +36,7 @@ template <int D>
 struct Fp4Shape {
   static constexpr int kWavesPer = D == 64 ? 8 : 4, kThreadsPer = kWavesPer * kWave;
   static constexpr int kPerCu = D == 64 ? 2 : 3;              // workgroups on a compute unit
-  static constexpr int kStages = D == 64 ? 3 : 2;             // fragments a wave has room for
+  static constexpr int kStages = 2;                           // fragments a wave has room for (three gain nothing)
   static constexpr int kResident = 256 * kPerCu;
   static_assert(kResident <= kFp4Counters, "a count for each");
   static constexpr int kMinShare = 16;                        // fragments a workgroup has at the least
@@ -483,8 +483,23 @@ void fp4_attention_kernel(Fp4Params p) {
       }
     }
     // the waves' results: head rows of channels, maximum, sum
-    const float l = rows_sum_f32(st.l);
-    if (head < p.G) {
+    float l = rows_sum_f32(st.l);
+    if constexpr (kNarrow) {      // the two halves of the columns first
+      auto other = [](float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kDppRowRor8, 0xf, 0xf, true)); };
+      const float top = raw_max(st.m, other(st.m)), a = __builtin_amdgcn_exp2f(st.m - (top == -INFINITY ? 0.f : top));
+      st.m = top;
+      l *= a;
+      l += other(l);
+#pragma unroll
+      for (int cb = 0; cb < D / 16; ++cb) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = st.acc[cb][i] * a;
+          st.acc[cb][i] = x + other(x);
+        }
+      }
+    }
+    if (r < p.G) {
       float* row = merge + wave * kWaveRows + r * kRow;
 #pragma unroll
       for (int cb = 0; cb < D / 16; ++cb) *reinterpret_cast<float4_t*>(row + 16 * cb + 4 * kb) = st.acc[cb];
@@ -503,16 +518,15 @@ void fp4_attention_kernel(Fp4Params p) {
     float* my_part = place(blockIdx.x);
     for (int i = tid; i < p.G * D; i += kFp4Threads) {
       const int g = i / D, c = i % D;
-      constexpr int kHalves = kNarrow ? 2 : 1;       // columns of a head
       float M = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kFp4Waves * kHalves; ++w) M = fmaxf(M, merge[w / kHalves * kWaveRows + (g + w % kHalves * 8) * kRow + D]);
+      for (int w = 0; w < kFp4Waves; ++w) M = raw_max(M, merge[w * kWaveRows + g * kRow + D]);
       // (a wave without a token has zeros and the weight 0; what is not a number stays so)
       const float ref = M == -INFINITY ? 0.f : M;
       float o = 0.f, sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kFp4Waves * kHalves; ++w) {
-        const float* row = merge + w / kHalves * kWaveRows + (g + w % kHalves * 8) * kRow;
+      for (int w = 0; w < kFp4Waves; ++w) {
+        const float* row = merge + w * kWaveRows + g * kRow;
         const float a = __builtin_amdgcn_exp2f(row[D] - ref);
         o += a * row[c];
         sum += a * row[D + 1];
