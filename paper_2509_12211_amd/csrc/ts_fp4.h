@@ -391,7 +391,7 @@ void fp4_attention_kernel(Fp4Params p) {
   {
     const uint32_t key = aligned ? blockIdx.x : blockIdx.x * share;       // workgroups, or fragments, are numbered through
     uint32_t from = 0;
-    if (!aligned && key >= total) return;
+    if (!aligned && (blockIdx.x >= room || key >= total)) return;      // (key: what 32 bits hold, of the first room)
     bool found = false;
     uint32_t frags_before = 0;
     for (int base = 0; base < p.B; base += kWave) {

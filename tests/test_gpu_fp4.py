@@ -336,6 +336,33 @@ def test_many_units(B, lens, Hq, Hkv, d):
     c.check(c.out, c.lse, 0.2, what="many")
 
 
+def test_equal_shares_of_more_long_units_than_workgroups():
+    """800 units of some 190 fragments: workgroups that reach over several units' ends.  The sequences'
+    tables are permutations of the same pages, so that the cache and its plain form stay small."""
+    g = torch.Generator().manual_seed(12)
+    B, Hq, Hkv, d, S, pages = 100, 16, 8, 64, 16, 400
+    one = Fp4([pages * S], Hq, Hkv, d, S, g)
+    perm = torch.stack([torch.randperm(pages, generator=g) for _ in range(B)])
+    table = one.table.cpu()[0].long()[perm].int().to(DEV)
+    n = torch.randint(5900, pages * S + 1, (B,), generator=g).int()
+    n[1], n[50] = 0, 1
+    lens = n.to(DEV)
+    box = torch.zeros((B, Hkv, pages, d), dtype=BF, device=DEV)
+    lay = ts.make_layout(B, Hq, Hkv, d, S, pages, one.pool, None, table, lens, box, box)
+    q = torch.randn((B, Hq, d), generator=g).to(BF).to(DEV)
+    out = torch.full((B, Hq, d), math.nan, device=DEV)
+    ws = ts.new_dense_workspace(lay, DEV)
+    ts.dense_decode_attention(lay, q, 0.125, out, ws)
+    assert torch.isfinite(out).all() and (out[1] == 0).all()
+    for b in (0, 1, 2, 33, 50, 51, 98, 99):
+        at = (perm[b][:, None] * S + torch.arange(S)).view(-1)[:int(n[b])]
+        want, _, bound = ref.attention(q[b].cpu(), one.k[0][:, at], one.v[0][:, at], 0.125)
+        assert ((out[b].cpu().double() - want).abs() <= bound).all(), b
+    again = torch.full_like(out, math.nan)
+    ts.dense_decode_attention(lay, q, 0.125, again, ws)
+    assert torch.equal(again, out)
+
+
 def test_what_is_not_a_number_stays_with_its_head():
     c = Fp4([3000, 17], 8, 2, 64, 16, torch.Generator().manual_seed(9))
     ws = ts.new_dense_workspace(c.layout, DEV)
