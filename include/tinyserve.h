@@ -141,7 +141,9 @@ typedef struct ts_layout {
    *                                 channel, the even token in a byte's low half;
    *                                 channel c is word [c/64][c%16][(c/16)%4]
    *   scales  bf16 [S] of the keys, then bf16 [S] of the values.
-   * page_size is at least 8.  Queries, appended tokens and metadata are bf16.
+   * page_size is at least 8.  Queries, appended tokens and metadata are bf16; an
+   * attention's queries are 16-byte aligned, its results 16-byte (fp32) or 8-byte
+   * (bf16).
    * Quantising a bf16 row: scale = max_c |x_c| / 6 in fp32, rounded up to bf16 (1 for
    * a zero row), code = x_c / scale in fp32, to the nearest number, ties to the even
    * code, no negative zero.  Rows should be finite: a NaN becomes 0, an infinity the

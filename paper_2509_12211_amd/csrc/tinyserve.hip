@@ -317,6 +317,11 @@ static int check_pool(const ts_layout* L) {
   return TS_OK;
 }
 
+// The queries and results of an attention over four bits, which travel by sixteen bytes.
+static int check_fp4_rows(const ts_layout* L, const void* q, const void* out) {
+  return aligned(q, 16) && aligned(out, L->out_format == TS_OUT_BF16 ? 8 : 16) ? TS_OK : TS_ERR_SHAPE;
+}
+
 static int tile_stride_of(const ts_layout* L) {
   if (L->kv_format == TS_KV_FP4) return L->kv_tile_stride ? L->kv_tile_stride : fp4_block_bytes(L);
   return L->kv_tile_stride ? L->kv_tile_stride : L->head_dim * L->page_size;
@@ -426,6 +431,7 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
   p.out = static_cast<float*>(out);
   p.lse = lse_out;
   p.part = reinterpret_cast<float*>(ws + pl.off_part);
+  p.part_ml = p.part + (size_t)pl.room * 2 * (L->num_q_heads / L->num_kv_heads) * L->head_dim;
   p.done = reinterpret_cast<int32_t*>(ws + pl.off_done);
   p.B = L->num_seqs;
   p.Hq = L->num_q_heads;
@@ -434,7 +440,6 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
   p.Pmax = L->max_pages_per_seq;
   p.Kmax = Kmax;
   p.n_phys = L->num_phys_pages;
-  p.out_bf16 = L->out_format == TS_OUT_BF16;
   p.room = pl.room;
   p.inv_room = 1.0f / (float)pl.room;
   p.tile_stride = tile_stride_of(L);
@@ -449,7 +454,7 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
   } while (0)
 #define TS_LAUNCH_FP4_OUT(DD, SS, SPARSE, NARROW)                \
   do {                                                           \
-    if (p.out_bf16) TS_LAUNCH_FP4(DD, SS, SPARSE, NARROW, false); \
+    if (L->out_format == TS_OUT_BF16) TS_LAUNCH_FP4(DD, SS, SPARSE, NARROW, false); \
     else TS_LAUNCH_FP4(DD, SS, SPARSE, NARROW, true);            \
   } while (0)
 #define TS_LAUNCH_FP4_HEADS(DD, SS, SPARSE)                      \
@@ -610,13 +615,15 @@ static int launch_fp4_query_aware(const ts_layout* layout, const void* k_new, co
                                   int32_t topk, const int32_t* topk_per_seq, int32_t max_topk, float softmax_scale,
                                   void* out, float* scores_out, int32_t* sel_out, int32_t* sel_count_out,
                                   void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_fp4_rows(layout, q, out);
+  if (st != TS_OK) return st;
   const Fp4Plan pl = make_fp4_plan(layout, max_topk, true);
   if (workspace_bytes < pl.total) return TS_ERR_WORKSPACE;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   float* scores = scores_out ? scores_out : reinterpret_cast<float*>(ws + pl.off_scores);
   int32_t* sel = sel_out ? sel_out : reinterpret_cast<int32_t*>(ws + pl.off_sel);
   int32_t* count = sel_count_out ? sel_count_out : reinterpret_cast<int32_t*>(ws + pl.off_count);
-  int st = k_new ? append_fp4_token(layout, k_new, v_new, 1, (hipStream_t)stream) : TS_OK;
+  st = k_new ? append_fp4_token(layout, k_new, v_new, 1, (hipStream_t)stream) : TS_OK;
   if (st == TS_OK) st = ts_score_pages(layout, q, scores, stream);
   if (st == TS_OK) st = ts_select_topk_pages(layout, scores, topk, topk_per_seq, max_topk, sel, count, stream);
   if (st != TS_OK) return st;
@@ -994,6 +1001,7 @@ int ts_sparse_decode_attention(const ts_layout* layout, const void* q, const int
   if ((st = check_pool(layout)) != TS_OK) return st;
   if (max_topk < 1) return TS_ERR_SHAPE;
   if (layout->kv_format == TS_KV_FP4) {
+    if ((st = check_fp4_rows(layout, q, out)) != TS_OK) return st;
     const Fp4Plan f = make_fp4_plan(layout, max_topk, true);
     if (workspace_bytes < f.attend_total) return TS_ERR_WORKSPACE;
     return launch_fp4_attention(layout, f, q, sel, sel_count, max_topk, softmax_scale, out, lse_out,
@@ -1020,6 +1028,7 @@ int ts_dense_decode_attention(const ts_layout* layout, const void* q, float soft
   if (!q || !out || !workspace) return TS_ERR_NULL;
   if ((st = check_pool(layout)) != TS_OK) return st;
   if (layout->kv_format == TS_KV_FP4) {
+    if ((st = check_fp4_rows(layout, q, out)) != TS_OK) return st;
     const Fp4Plan f = make_fp4_plan(layout, layout->max_pages_per_seq, false);
     if (workspace_bytes < f.total) return TS_ERR_WORKSPACE;
     return launch_fp4_attention(layout, f, q, nullptr, nullptr, 0, softmax_scale, out, lse_out,

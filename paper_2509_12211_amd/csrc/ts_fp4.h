@@ -57,9 +57,10 @@ struct Fp4Params {
   const int32_t *sel, *sel_count;   // sparse: [B][Hkv][Kmax], [B]
   float* out;                       // [B][Hq][D] fp32 or bf16
   float* lse;                       // nullable [B][Hq]
-  float* part;                      // [room][2][G][D + 2]: what a unit's workgroups hand over
+  float* part;                      // [room][2][G][D]: what a unit's workgroups hand over, and
+  float* part_ml;                   // [room][2][G][2]: the maximum and sum that go with it
   int32_t* done;                    // [room] by a shared unit's first workgroup: how many have; zero between launches
-  int B, Hq, Hkv, G, Pmax, Kmax, n_phys, out_bf16;
+  int B, Hq, Hkv, G, Pmax, Kmax, n_phys;
   int room;                         // workgroups that have a place in part, and are at work at once
   long long tile_stride;
   float scale_log2, inv_room;
@@ -319,9 +320,20 @@ __device__ __forceinline__ int fp4_frags(const Fp4Params& p, int b) {
   return (len + kFp4Frag - 1) / kFp4Frag;
 }
 
-__device__ __forceinline__ void store_fp4_out(const Fp4Params& p, size_t idx, float v) {
-  if (p.out_bf16) reinterpret_cast<uint16_t*>(p.out)[idx] = f32_to_bf16_rn(v);
-  else p.out[idx] = v;
+template <bool kOut32>
+__device__ __forceinline__ void store_fp4_out(const Fp4Params& p, size_t idx, const float4_t& v) {
+  if constexpr (kOut32) *reinterpret_cast<float4_t*>(p.out + idx) = v;
+  else
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.out) + idx) =
+        make_uint2(pack_elems<false>(v[0], v[1]), pack_elems<false>(v[2], v[3]));
+}
+// Partial results travel by 16 bytes past the caches (as store_agent and load_agent do by four).
+constexpr int kPartAgent = 16;      // cache policy: agent scope
+__device__ __forceinline__ void store_part(__amdgpu_buffer_rsrc_t r, uint32_t at, const float4_t& v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(stream_u4, v), r, (int)at, 0, kPartAgent);
+}
+__device__ __forceinline__ float4_t load_part(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+  return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, kPartAgent));
 }
 
 template <int D, int S, bool kSparse, bool kNarrow, bool kOut32>
@@ -333,7 +345,7 @@ void fp4_attention_kernel(Fp4Params p) {
   constexpr int kFrags = (kFp4List + 1 - FPP) * FPP / PPF;   // fragments the list in LDS covers, begun within a page too
   constexpr int kRow = D + 4;                        // a head's merged row: channels, maximum, sum
   constexpr int kWaveRows = Shape::kRing / 4;        // a wave's rows lie where its fragments were
-  static_assert(16 * kRow <= kWaveRows, "room for a wave's rows");
+  static_assert(16 * kRow <= kWaveRows && kRow % 4 == 0 && kWaveRows % 4 == 0, "room for a wave's rows");
   extern __shared__ __align__(16) unsigned char smem[];
   Fp4Entry* list = reinterpret_cast<Fp4Entry*>(smem);
   float* merge = reinterpret_cast<float*>(list + kFp4List);
@@ -355,7 +367,8 @@ void fp4_attention_kernel(Fp4Params p) {
       while (none != 0) {
         const int e = base + __builtin_ctzll(none);
         none &= none - 1;
-        for (int x = lane; x < p.Hq * D; x += kWave) store_fp4_out(p, (size_t)e * p.Hq * D + x, 0.f);
+        for (int x = 4 * lane; x < p.Hq * D; x += 4 * kWave)
+          store_fp4_out<kOut32>(p, (size_t)e * p.Hq * D + x, float4_t{0.f, 0.f, 0.f, 0.f});
         if (p.lse)
           for (int x = lane; x < p.Hq; x += kWave) p.lse[(size_t)e * p.Hq + x] = -INFINITY;
       }
@@ -514,32 +527,40 @@ void fp4_attention_kernel(Fp4Params p) {
     const int parts = aligned ? parts_of_unit : (int)((uend - 1) / share - w0) + 1;
     const bool whole = parts == 1;
     // (one that reaches into two units it shares with others has a place for either)
-    auto place = [&](uint32_t w) { return p.part + ((size_t)w * 2 + (aligned || w * share > ustart ? 0 : 1)) * p.G * (D + 2); };
-    float* my_part = place(blockIdx.x);
-    for (int i = tid; i < p.G * D; i += kFp4Threads) {
-      const int g = i / D, c = i % D;
+    auto place = [&](uint32_t w) { return (w * 2 + (aligned || w * share > ustart ? 0u : 1u)) * (uint32_t)p.G; };   // rows
+    const __amdgpu_buffer_rsrc_t part = __builtin_amdgcn_make_buffer_rsrc(p.part, (short)0, p.room * 2 * p.G * D * 4, 0x00020000);
+    const int items = p.G * (D / 4);                       // four channels of a head
+    auto finish = [&](int item, float M, float sum, float4_t o) {
+      const int g = item / (D / 4), c = item % (D / 4) * 4;
+      const size_t at_head = (size_t)b * p.Hq + h * p.G + g;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      store_fp4_out<kOut32>(p, at_head * D + c, o * inv);
+      if (p.lse && c == 0) p.lse[at_head] = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * 0.6931471805599453f;
+    };
+    for (int i = tid; i < items; i += kFp4Threads) {
+      const int g = i / (D / 4), c = i % (D / 4) * 4;
       float M = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kFp4Waves; ++w) M = raw_max(M, merge[w * kWaveRows + g * kRow + D]);
       // (a wave without a token has zeros and the weight 0; what is not a number stays so)
       const float ref = M == -INFINITY ? 0.f : M;
-      float o = 0.f, sum = 0.f;
+      float4_t o = {0.f, 0.f, 0.f, 0.f};
+      float sum = 0.f;
 #pragma unroll
       for (int w = 0; w < kFp4Waves; ++w) {
         const float* row = merge + w * kWaveRows + g * kRow;
         const float a = __builtin_amdgcn_exp2f(row[D] - ref);
-        o += a * row[c];
+        o += a * *reinterpret_cast<const float4_t*>(row + c);
         sum += a * row[D + 1];
       }
       if (whole) {
-        const size_t at_head = (size_t)b * p.Hq + h * p.G + g;
-        store_fp4_out(p, at_head * D + c, sum == 0.f ? 0.f : o / sum);
-        if (p.lse && c == 0) p.lse[at_head] = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * 0.6931471805599453f;
+        finish(i, M, sum, o);
       } else {
-        store_agent(my_part + g * (D + 2) + c, o);
+        const uint32_t row = place(blockIdx.x) + (uint32_t)g;
+        store_part(part, (row * D + (uint32_t)c) * 4u, o);
         if (c == 0) {
-          store_agent(my_part + g * (D + 2) + D, M);
-          store_agent(my_part + g * (D + 2) + D + 1, sum);
+          store_agent(p.part_ml + 2 * row, M);
+          store_agent(p.part_ml + 2 * row + 1, sum);
         }
       }
     }
@@ -553,19 +574,21 @@ void fp4_attention_kernel(Fp4Params p) {
       }
       __syncthreads();
       if (uniform(last_one)) {
-        // (a part's maximum, sum and number asked for together, eight parts at a time)
-        for (int i = tid; i < p.G * D; i += kFp4Threads) {
-          const int g = i / D, c = i % D;
+        // (a part's maximum, sum and numbers asked for together, eight parts at a time)
+        for (int i = tid; i < items; i += kFp4Threads) {
+          const int g = i / (D / 4), c = i % (D / 4) * 4;
           constexpr int kAhead = 8;
-          float M = -INFINITY, o = 0.f, sum = 0.f;
+          float M = -INFINITY, sum = 0.f;
+          float4_t o = {0.f, 0.f, 0.f, 0.f};
           for (int e0 = 0; e0 < parts; e0 += kAhead) {
-            float m[kAhead], x[kAhead], z[kAhead];
+            float m[kAhead], z[kAhead];
+            float4_t x[kAhead];
 #pragma unroll
             for (int e = 0; e < kAhead; ++e) {
-              const float* part = place(w0 + (uint32_t)min(e0 + e, parts - 1)) + g * (D + 2);
-              m[e] = load_agent(part + D);
-              x[e] = load_agent(part + c);
-              z[e] = load_agent(part + D + 1);
+              const uint32_t row = place(w0 + (uint32_t)min(e0 + e, parts - 1)) + (uint32_t)g;
+              x[e] = load_part(part, (row * D + (uint32_t)c) * 4u);
+              m[e] = load_agent(p.part_ml + 2 * row);
+              z[e] = load_agent(p.part_ml + 2 * row + 1);
             }
             float top = M;
 #pragma unroll
@@ -581,9 +604,7 @@ void fp4_attention_kernel(Fp4Params p) {
             }
             M = top;
           }
-          const size_t at_head = (size_t)b * p.Hq + h * p.G + g;
-          store_fp4_out(p, at_head * D + c, sum == 0.f ? 0.f : o / sum);
-          if (p.lse && c == 0) p.lse[at_head] = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * 0.6931471805599453f;
+          finish(i, M, sum, o);
         }
       }
     }

@@ -171,6 +171,11 @@ def test_four_bit_calls_check_their_pointers_and_workspaces():
     assert L.ts_append_and_decode(by, P, P, P, 8, None, 8, 1.0, P, None, None, None, P, aware - 1, None) == ts.TS_ERR_WORKSPACE
     assert L.ts_sparse_decode_attention(by, P, P, P, 8, 1.0, P, None, P, 16, None) == ts.TS_ERR_WORKSPACE
     assert L.ts_query_aware_decode_static(by, P, 8, None, 8, 1.0, P, None, None, None, None) == ts.TS_ERR_UNSUPPORTED
+    for q, out, bf16 in ((P + 8, P, 0), (P, P + 8, 0), (P, P + 4, 1)):       # rows that do not lie on their bytes
+        by_ = ctypes.byref(fp4(out_format=bf16))
+        assert L.ts_dense_decode_attention(by_, q, 1.0, out, None, P, big, None) == ts.TS_ERR_SHAPE
+        assert L.ts_sparse_decode_attention(by_, q, P, P, 8, 1.0, out, None, P, big, None) == ts.TS_ERR_SHAPE
+        assert L.ts_append_and_decode(by_, P, P, q, 8, None, 8, 1.0, out, None, None, None, P, big, None) == ts.TS_ERR_SHAPE
     assert L.ts_query_aware_decode(by, P, 9, None, 8, 1.0, P, None, None, None, P, big, None) == ts.TS_ERR_SHAPE
 
 
