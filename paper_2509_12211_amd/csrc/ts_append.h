@@ -476,8 +476,8 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
           rotate_row<D, kHalf>(p.r, lanes.turns, qn, ang, qa[i], qb[i]);
           const int g = g0 + (round + i) * step;
           if (g < G) {
-            *reinterpret_cast<uint2*>(q_dst + g * D + lanes.c0) = qa[i];
-            *reinterpret_cast<uint2*>(q_dst + g * D + lanes.c1) = qb[i];
+            stream_row(q_dst + g * D + lanes.c0, qa[i]);
+            stream_row(q_dst + g * D + lanes.c1, qb[i]);
           }
         }
       round += kAhead;
