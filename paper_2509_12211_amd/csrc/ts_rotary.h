@@ -116,10 +116,10 @@ __device__ __forceinline__ uint32_t pack_elems(float x, float y) {
 }
 
 // 1 / sqrt(m): the instruction's estimate y (good to 2^-22 or better), and with e = 1 - m y^2 the series
-// y (1 + e / 2 + 3 e^2 / 8), which leaves the last bits of fp64.
+// y (1 + e / 2 + 3 e^2 / 8), which leaves the last bits of fp64.  (m infinite or 0: y itself, and e is no number.)
 __device__ __forceinline__ double inverse_root(double m) {
   const double y = __builtin_amdgcn_rsq(m), e = fma(-m * y, y, 1.0);
-  return fma(y * e, fma(0.375, e, 0.5), y);
+  return e == e ? fma(y * e, fma(0.375, e, 0.5), y) : y;
 }
 
 // One row, eight channels a lane: normed, rotated and rounded to 16 bits.  All lanes of the row take part.

@@ -102,6 +102,28 @@ def test_rows_at_the_edges_of_their_type():
     assert torch.equal(out.view(torch.int16), x.view(torch.int16))
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_that_hold_infinities_and_what_is_not_a_number(d, dtype):
+    """By the formula: an infinity's row is zero but for the infinity itself, 0 / 0 and NaN go where they go."""
+    x = torch.randn((4, 2, d), generator=torch.Generator().manual_seed(d)).to(dtype)
+    x[0, 0, 9] = math.inf
+    x[1, 1, 2], x[1, 1, 40] = -math.inf, math.inf
+    x[2, 0, 5] = math.nan
+    x[3, 0] = 0
+    for table in (None, ts.rotary_table(10, 32, device=DEV)):
+        pos = torch.tensor([3, 0, 9, 4], dtype=torch.int32)
+        w, out = torch.ones(d, device=DEV), torch.empty((4, 2, d), dtype=dtype, device=DEV)
+        r = ts.make_rotary(table, positions=None if table is None else pos.to(DEV), q_norm=w, norm_eps=0.0)
+        ts.rotate_rows(r, x.to(DEV), None, out)
+        exact, slack = ref.rotated(x, w.cpu(), 0.0, None if table is None else table.cpu(),
+                                   pos.long()[:, None].expand(-1, 16), False)
+        got = out.cpu().double()
+        assert torch.equal(got.isnan(), exact.isnan())
+        on = ~exact.isnan()
+        assert ((got - exact).abs() <= ref.row_bound(exact, slack, dtype))[on].all()
+
+
 # ------------------------------------------------------------------------------------------- append
 class Cache:
     """A paged cache of any format with its boxes, what it holds, and room for more."""
