@@ -286,6 +286,8 @@ def rotate_rows(rotary, q, k, q_out=None, k_out=None):
         kop = kp
         if k_out is not None:
             kos, kop = _row_stride(k_out, shape, dtype, device, where), k_out.data_ptr()
+    if n == 0:        # (rows of no tokens have no address)
+        return
     rows = _pack_rows(n, _ROW_FORMATS[dtype], qp, kp, 0, qop, kop, qs, ks, 0, qos, kos)
     _check(lib().ts_rotate_rows(ctypes.byref(rotary), rows, Hq, Hkv, d, _stream_on(device, where)), where)
 
@@ -317,6 +319,8 @@ def append_rows(layout, k, v, rotary=None, q=None, q_out=None, cu_tokens=None, a
         qs = qos = _row_stride(q, shape, dtype, device, where)
         if q_out is not None:
             qos, qop = _row_stride(q_out, shape, dtype, device, where), q_out.data_ptr()
+    if n == 0:
+        return
     lens = TS_LENS_AFTER if lens_include_new else TS_LENS_ADVANCE if advance_seq_lens else TS_LENS_KEEP
     rows = _pack_rows(n, 0, qp, k.data_ptr(), v.data_ptr(), qop, 0, qs, ks, vs, qos, 0)
     _check(lib().ts_append_rows(ctypes.byref(layout), ref, rows, None if cu_tokens is None else cu_tokens.data_ptr(),

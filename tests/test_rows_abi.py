@@ -212,6 +212,15 @@ def test_binding_refuses_tensors_that_do_not_fit():
             call()
 
 
+def test_rows_of_no_tokens_are_no_work():
+    """(An empty tensor has no address, and nothing is enqueued: this runs where there is no GPU.)"""
+    none = torch.empty((0, 8, 64), dtype=torch.bfloat16)
+    ts.rotate_rows(ts.make_rotary(), none, none[:, :2])
+    ts.append_rows(layout(), none[:, :2], none[:, :2], q=none[:, :8], cu_tokens=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ts.TinyServeError):
+        ts.rotate_rows(ts.make_rotary(), none, none.half())
+
+
 def test_reference_four_bit_numbers():
     """The plain form itself: every code is its own nearest, ties go to even codes, the largest number of
     a row is kept by the scale that it sets, and packing is undone by unpacking."""
