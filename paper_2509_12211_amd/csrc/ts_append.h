@@ -234,7 +234,8 @@ struct PageTiles {
 // One token for each sequence: every row by itself, eight or sixteen lanes for each, no LDS and no barrier.
 // A key's lanes widen or open its page's box in the channels they hold; a value's lanes put its eight
 // numbers into their places in the channel-major tile.  Bound by a chain of trips to memory (length,
-// block-table entry and angles, box); the row itself is asked for ahead of them.
+// block-table entry and angles, box); the row itself is asked for ahead of them.  64 sequences, 32 KV and 32
+// query heads of 128 channels in bf16, 4.2 MB: 5.8 us; one sequence, 4 bits: 4.3.
 // grid (sequences, row groups): rows 0 .. Hkv - 1 keys, then values, then queries.
 template <int FMT, int D>
 __global__ __launch_bounds__(kRotaryThreads) void append_token_rows_kernel(AppendParams p) {
@@ -372,6 +373,10 @@ __device__ __forceinline__ float over_groups(float v) {
 // the vector unit (some hundred instructions a row), so the box is worked out where that takes the fewest: with
 // 16 bits from the keys in LDS, two channels a thread; quantised, from the numbers that the lanes hold anyway, over
 // the wave's groups and then, in LDS, over the waves.
+// Four waves on a SIMD: five and six spill (169 and 231 us where this takes 82).  Two query rows on their way at a
+// time: one takes 89.7 us, three 88.6; the queries in workgroups of their own 100.
+// Seven prompts of 14 400 tokens in all, 32 and 8 heads of 128 channels, bf16, 354.9 MB: 82 us, 4.3 TB/s; five of
+// 6 700, into 4 bits, 145.4 MB: 37.4 us, 3.9 TB/s, the quantiser's instructions on top.
 template <int FMT, int D>
 __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendParams p) {
   constexpr bool kHalf = FMT == kPoolFp16;

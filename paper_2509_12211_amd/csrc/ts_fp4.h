@@ -4,9 +4,9 @@
 // launch.  Fragments of 32 tokens: K (16 tokens x 32 channels a product) and V (16 channels x 32 tokens) are
 // expanded to bf16 in registers, one instruction for two codes, and go through v_mfma_f32_16x16x32_bf16;
 // the scales of 32 tokens multiply the logits (K) and the softmax weights (V) afterwards.  e2m1 numbers and
-// bf16 queries are exact operands; the weights go in as three bf16 numbers (the nearest, the remainder's
-// nearest, and what is left: 2^-27 relative; with two an fp32 output was 2e-6 off, twice what the sums
-// cost), so nothing but the fp32 sums rounds.
+// bf16 queries are exact operands.  For an fp32 output the weights go in as three bf16 numbers (the nearest, the
+// remainder's nearest, and what is left, which fits: 24 bits in all; with two it was 2e-6 off, twice what the sums
+// cost), so nothing but the fp32 sums rounds; for a bf16 output as two, 2^-17, far below its own rounding of 2^-8.
 //   logits  St[token][head] = K[token][:] . Q^T[:][head]      row = token, column = head
 //   output  Ot[chan][head] += V^T[chan][token] . P^T[token][head]
 // Row 4 kb + i of logit tile t is token 8 kb + 4 t + i of the fragment (kb: quarter of the wave), so the eight
@@ -17,6 +17,11 @@
 // unit by unit, each to as many workgroups as its length asks for.  A workgroup's waves take the fragments of a
 // unit in turn and merge in LDS.  A unit that several workgroups share is merged by the
 // last of them to arrive (an atomic count in the workspace, set back to zero); nobody waits.
+//
+// Measured (kernel alone, cold data): 64 sequences of 1024 to 32768 tokens, 8 KV heads of 128 channels, 1.14 GB:
+// 216 us, 5.3 TB/s, bound by memory.  16 sequences of 16384 tokens, 4 KV heads of 64, 71.5 MB: 21.2 us, 3.4 TB/s:
+// each wave has eight fragments, and the way to the first (lengths, table, block) and the merge are a third of
+// the time.  One sequence of 4096 tokens and one head, 0.28 MB: 7.8 us, that chain alone.
 #pragma once
 #include "ts_append.h"
 #include "ts_attend.h"
@@ -25,21 +30,28 @@ namespace ts {
 
 constexpr int kFp4Frag = 32;            // tokens of a fragment
 constexpr int kFp4List = 1024;          // list entries held in LDS at a time
-constexpr int kFp4Parts = 64;           // about how many workgroups share a unit at the most
+// About how many workgroups share a unit at the most: the last one merges them all.  32, 64, 96 and 128 take, for
+// one sequence of 131072 tokens, 8 heads on one of 64 channels, 21.9, 18.4, 19.6 and 21.9 us; for one of 262144,
+// 16 heads on one of 128 channels, 48 to 50 us from 64 on.
+constexpr int kFp4Parts = 64;
 constexpr int kFp4Counters = 1024;      // places for counts, whatever the batch
-constexpr uint32_t kFp4LongShare = 192; // fragments of a workgroup from which on all get the same number
+// Fragments of a workgroup from which on all get the same number: with 384 the ragged batch of 1.1 GB goes unit by
+// unit and takes 250 us instead of 222; 48 changes nothing that was measured.
+constexpr uint32_t kFp4LongShare = 192;
 
-// Workgroups of eight waves, two on a compute unit, for 64 channels; with 128, where a wave's registers leave
-// room for three on a SIMD and no less, of four, three on a unit (ragged batch of 1.1 GB 232 -> 223 us, lists of
-// a quarter of the pages 23.2 -> 20.5; with 64 channels the smaller ones lose, 24.3 -> 28.8 and 11.9 -> 15.6).
+// Workgroups of eight waves, two on a compute unit, for 64 channels (71.5 MB 21.7 us; three of them 24.7, four of
+// four waves 26.0).  With 128, where a wave's registers leave room for three on a SIMD and no less, of four waves,
+// three on a unit (1.1 GB 220 us, lists of a quarter of the pages 15.2; two of eight waves 223 and 16.0).
 template <int D>
 struct Fp4Shape {
   static constexpr int kWavesPer = D == 64 ? 8 : 4, kThreadsPer = kWavesPer * kWave;
   static constexpr int kPerCu = D == 64 ? 2 : 3;              // workgroups on a compute unit
-  static constexpr int kStages = 2;                           // fragments a wave has room for (three gain nothing)
+  static constexpr int kStages = 2;                           // fragments a wave has room for (three: 22.4 us where two take 21.7)
   static constexpr int kResident = 256 * kPerCu;
   static_assert(kResident <= kFp4Counters, "a count for each");
-  static constexpr int kMinShare = 16;                        // fragments a workgroup has at the least
+  // Fragments a workgroup has at the least: with 8 one sequence of 3000 tokens takes 8.9 us, with 16 8.5, with 32
+  // 10.7; lists of a quarter of the pages 15.1 with 8, 14.3 with 16.
+  static constexpr int kMinShare = 16;
   // a fragment in LDS: keys, values, scales
   static constexpr int kKeys = 0, kValues = 16 * D, kScales = 32 * D, kStage = 32 * D + 256;
   static constexpr int kLoads = D / 32 + 1;                   // loads that bring it
@@ -623,7 +635,8 @@ void fp4_attention_kernel(Fp4Params p) {
 
 // Rebuild of the boxes: a page's D / 32 lanes own 32 channels each (16 bytes of a token's row) and walk
 // down its tokens, eight rows and their scales asked for together.  code * scale is exact in fp32, so the extremes
-// are, and are rounded outwards to bf16.  Bound by memory.
+// are, and are rounded outwards to bf16.  Bound by memory: 32 sequences of 16384 tokens, 8 KV heads of 128 channels,
+// 103 us, 4.0 TB/s (key codes and scales, 16 tokens a page; 4.6 with pages of 64); 16 of them with 4 of 64, 17.2 us.
 template <int D>
 __global__ __launch_bounds__(kThreads) void build_page_meta_fp4_kernel(MetaParams p) {
   constexpr int LPP = D / 32, PPW = kWave / LPP;    // lanes a page, pages a wave
