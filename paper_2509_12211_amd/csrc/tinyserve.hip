@@ -569,7 +569,8 @@ static int launch_append_rows(const ts_layout* L, const ts_rotary* rotary, const
       const size_t lds = AppendLds<FMT, DD>::bytes(p.S);                                      \
       /* pages that n tokens touch: at most (n - 1) / S + 2 */                                \
       const long long pages = (long long)p.T / p.S + 2LL * p.B;                               \
-      const dim3 grid((unsigned)pages, (unsigned)p.Hkv);                                      \
+      const long long z = (pages + 65534) / 65535;      /* (what a grid's second side holds) */ \
+      const dim3 grid((unsigned)p.Hkv, (unsigned)((pages + z - 1) / z), (unsigned)z);         \
       append_rows_kernel<FMT, DD><<<grid, kRotaryThreads, lds, stream>>>(p);                  \
     } else {                                                                                  \
       const int groups = kRotaryThreads / (DD / 8), n = 2 * p.Hkv + (p.q ? p.Hq : 0);         \

@@ -368,14 +368,15 @@ __device__ __forceinline__ float over_groups(float v) {
   return take(__uint_as_float(r.x), __uint_as_float(r.y));
 }
 
-// grid (touched pages or more, Hkv).  A token's key, value and queries are dealt to as many groups of
+// grid (Hkv, touched pages or more): the heads of a page one behind the other, as they lie in the projection's rows
+// and in the pool (bf16 prompts 73.5 us; the pages of a head one behind the other 81.5).  A token's key, value and queries are dealt to as many groups of
 // lanes as the workgroup has for each token, the rows asked for ahead of the lookups.  Half of the time goes to
 // the vector unit (some hundred instructions a row), so the box is worked out where that takes the fewest: with
 // 16 bits from the keys in LDS, two channels a thread; quantised, from the numbers that the lanes hold anyway, over
 // the wave's groups and then, in LDS, over the waves.
-// Four waves on a SIMD: five and six spill (169 and 231 us where this takes 82).  Two query rows on their way at a
-// time: one takes 89.7 us, three 88.6; the queries in workgroups of their own 100.
-// Seven prompts of 14 400 tokens in all, 32 and 8 heads of 128 channels, bf16, 354.9 MB: 82 us, 4.3 TB/s; five of
+// Four waves on a SIMD: five and six spill (twice and three times the time).  Two query rows on their way at a time:
+// one and three take 8 % longer; the queries in workgroups of their own 15 %.
+// Seven prompts of 14 400 tokens in all, 32 and 8 heads of 128 channels, bf16, 354.9 MB: 73.5 us, 4.8 TB/s; five of
 // 6 700, into 4 bits, 145.4 MB: 37.4 us, 3.9 TB/s, the quantiser's instructions on top.
 template <int FMT, int D>
 __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendParams p) {
@@ -387,9 +388,9 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
   Elem* vs = reinterpret_cast<Elem*>(smem);                                                  // [S][kRow]
   Elem* ks = Lds::kWide ? vs + (size_t)p.S * Lds::kRow : vs;                                 // 16 bits: [S][kRow]
   float* box = reinterpret_cast<float*>(ks + (size_t)p.S * Lds::kRow);                       // [2][parts][D]
-  const int sh = __builtin_ctz(p.S), h = blockIdx.y, tid = threadIdx.x;
+  const int sh = __builtin_ctz(p.S), h = blockIdx.x, tid = threadIdx.x;
   int b, j;
-  if (!find_page(p, sh, blockIdx.x, b, j)) return;
+  if (!find_page(p, sh, blockIdx.z * gridDim.y + blockIdx.y, b, j)) return;
   const int c0 = min(max(p.cu[b], 0), p.T), n = uniform(min(max(p.cu[b + 1], 0), p.T) - c0);
   const int len = uniform(p.seq_lens[b] - (p.lens_after ? p.cu[b + 1] - p.cu[b] : 0));
   if (len < 0) return;                                   // (no such length)

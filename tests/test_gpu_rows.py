@@ -402,6 +402,34 @@ def test_many_sequences_of_few_tokens():
     assert_cache(c, held, "few tokens")
 
 
+def test_more_pages_than_one_side_of_a_grid_holds():
+    """40000 sequences of three tokens that get none, one or two: half of them reach into a second page."""
+    g = torch.Generator().manual_seed(40)
+    B, S, d = 40000, 4, 64
+    n = torch.randint(0, 3, (B,), generator=g)
+    cu = torch.zeros(B + 1, dtype=torch.int64)
+    cu[1:] = n.cumsum(0)
+    T = int(cu[-1])
+    table = torch.randperm(2 * B, generator=g).view(B, 2)
+    k, v = (torch.randn((T, 1, d), generator=g).to(BF) for _ in range(2))
+    kp, vp = (torch.zeros((2 * B, 1, S * d), dtype=BF, device=DEV) for _ in range(2))
+    box = [torch.zeros((B, 1, 2, d), dtype=BF, device=DEV) for _ in range(2)]
+    lens = torch.full((B,), 3, dtype=torch.int32, device=DEV)
+    on_gpu = table.int().to(DEV)       # (held: a layout has addresses)
+    lay = ts.make_layout(B, 1, 1, d, S, 2, kp, vp, on_gpu, lens, *box)
+    ts.append_rows(lay, k.to(DEV), v.to(DEV), cu_tokens=cu.int().to(DEV))
+    seq = torch.repeat_interleave(torch.arange(B), n)
+    at = 3 + torch.arange(T) - cu[seq]
+    page, slot = table[seq, at // S], at % S
+    want_k, want_v = torch.zeros((2 * B, S, d), dtype=BF), torch.zeros((2 * B, d, S), dtype=BF)
+    want_k[page, slot], want_v[page, :, slot] = k[:, 0], v[:, 0]
+    assert torch.equal(kp.cpu().view(2 * B, S, d), want_k) and torch.equal(vp.cpu().view(2 * B, d, S), want_v)
+    assert torch.equal(lens.cpu(), (3 + n).int())
+    new = slot == 0                                            # (a page of one token: its box is the token)
+    for side in box:
+        assert torch.equal(side.cpu()[seq[new], 0, 1], k[new, 0])
+
+
 def test_appends_on_another_stream_and_captured():
     """A captured append replayed with other rows in the same buffers, eager work between the replays."""
     g = torch.Generator().manual_seed(11)
