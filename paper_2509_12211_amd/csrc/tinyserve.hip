@@ -567,9 +567,9 @@ static int launch_append_rows(const ts_layout* L, const ts_rotary* rotary, const
   do {                                                                                        \
     if (cu) {                                                                                 \
       const size_t lds = AppendLds<FMT, DD>::bytes(p.S);                                      \
-      /* pages that n tokens touch: at most (n - 1) / S + 2 */                                \
+      /* tasks, of which n tokens have n / S + 2 */                                           \
       const long long pages = (long long)p.T / p.S + 2LL * p.B;                               \
-      const long long z = (pages + 65534) / 65535;      /* (what a grid's second side holds) */ \
+      const long long z = (pages + 65534) / 65535;   /* a grid's second side holds 65535 */   \
       const dim3 grid((unsigned)p.Hkv, (unsigned)((pages + z - 1) / z), (unsigned)z);         \
       append_rows_kernel<FMT, DD><<<grid, kRotaryThreads, lds, stream>>>(p);                  \
     } else {                                                                                  \

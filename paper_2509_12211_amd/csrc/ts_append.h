@@ -327,33 +327,23 @@ __global__ __launch_bounds__(kRotaryThreads) void append_token_rows_kernel(Appen
   }
 }
 
-// Which page of which sequence workgroup `task` has.  The sequences' touched pages are numbered through;
-// every wave works the same answer out.  False: there are fewer.
-__device__ __forceinline__ bool find_page(const AppendParams& p, int sh, int task, int& b, int& j) {
-  int before = 0;
-  for (int base = 0; base < p.B; base += kWave) {
-    const int i = base + lane_id();
-    int pages = 0, first = 0;
-    if (i < p.B) {
-      const int c0 = min(max(p.cu[i], 0), p.T), c1 = min(max(p.cu[i + 1], 0), p.T), n = c1 - c0;
-      if (n > 0) {
-        const int len = p.seq_lens[i] - (p.lens_after ? p.cu[i + 1] - p.cu[i] : 0);
-        first = len >> sh;
-        pages = ((len + n - 1) >> sh) - first + 1;
-      }
-    }
-    const int upto = before + wave_inclusive_sum(pages);
-    const uint64_t mine = __ballot(task < upto && task >= upto - pages);
-    if (mine != 0) {
-      const int src = __builtin_ctzll(mine);
-      b = base + src;
-      j = __builtin_amdgcn_readlane(first, src) + task - __builtin_amdgcn_readlane(upto - pages, src);
-      b = uniform(b);
-      return true;
-    }
-    before = __builtin_amdgcn_readlane(upto, kWave - 1);
+// Sequence b's new tokens begin at row first_row(b), and its pages are the tasks from first_task(b) on: n tokens touch at most
+// n / S + 2 pages (rounded down), so the sequences' tasks do not overlap whatever their lengths.
+__device__ __forceinline__ int first_row(const AppendParams& p, int b) { return min(max(p.cu[b], 0), p.T); }
+__device__ __forceinline__ int first_task(int row, int sh, int b) { return (row >> sh) + 2 * b; }
+// The last sequence whose tasks begin at or before `task`, sixty-four looked at at a time: one trip to memory for up to
+// 64 sequences, two for 4096.  (Their pages counted and numbered through took a trip for every 64: 1024 sequences of
+// one token 93 us.)
+__device__ __forceinline__ int sequence_of(const AppendParams& p, int sh, int task) {
+  int b = 0;
+  for (int n = p.B; n > 1;) {
+    const int step = (n + kWave - 1) / kWave, i = lane_id() * step;
+    const uint64_t begun = __ballot(i < n && first_task(first_row(p, b + min(i, n - 1)), sh, b + i) <= task);
+    const int skip = max((int)__builtin_popcountll(begun) - 1, 0) * step;
+    b += skip;
+    n = min(step, n - skip);
   }
-  return false;
+  return uniform(b);
 }
 
 // Minimum or maximum of a value over the lanes of the wave that hold the same channels.
@@ -389,11 +379,11 @@ __global__ __launch_bounds__(kRotaryThreads, 4) void append_rows_kernel(AppendPa
   Elem* ks = Lds::kWide ? vs + (size_t)p.S * Lds::kRow : vs;                                 // 16 bits: [S][kRow]
   float* box = reinterpret_cast<float*>(ks + (size_t)p.S * Lds::kRow);                       // [2][parts][D]
   const int sh = __builtin_ctz(p.S), h = blockIdx.x, tid = threadIdx.x;
-  int b, j;
-  if (!find_page(p, sh, blockIdx.z * gridDim.y + blockIdx.y, b, j)) return;
-  const int c0 = min(max(p.cu[b], 0), p.T), n = uniform(min(max(p.cu[b + 1], 0), p.T) - c0);
+  const int task = blockIdx.z * gridDim.y + blockIdx.y, b = sequence_of(p, sh, task);
+  const int c0 = first_row(p, b), n = uniform(first_row(p, b + 1) - c0);
   const int len = uniform(p.seq_lens[b] - (p.lens_after ? p.cu[b + 1] - p.cu[b] : 0));
-  if (len < 0) return;                                   // (no such length)
+  const int page = uniform(task - first_task(c0, sh, b)), j = (len >> sh) + page;
+  if (n <= 0 || len < 0 || page < 0 || j > (len + n - 1) >> sh) return;      // (a task without a page, or no such length)
   const int p0 = max(j << sh, len), p1 = min((j + 1) << sh, len + n);   // positions of this page's new tokens
   const int ntok = uniform(p1 - p0), slot0 = p0 - (j << sh), tok0 = c0 + p0 - len;
   const bool fits = (long long)len + n <= (long long)p.Pmax << sh;
