@@ -445,12 +445,17 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
   p.tile_stride = tile_stride_of(L);
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
   int st = TS_OK;
-#define TS_LAUNCH_FP4(DD, SS, SPARSE, NARROW, OUT)                                 \
+#define TS_LAUNCH_FP4_BATCH(DD, SS, SPARSE, NARROW, OUT, MANY)                     \
   do {                                                                             \
     constexpr size_t lds = Fp4Shape<DD>::lds();                                    \
-    const auto kernel = fp4_attention_kernel<DD, SS, SPARSE, NARROW, OUT>;         \
+    const auto kernel = fp4_attention_kernel<DD, SS, SPARSE, NARROW, OUT, MANY>;   \
     if ((st = allow_lds(kernel, lds)) != TS_OK) return st;                         \
     kernel<<<pl.workgroups, Fp4Shape<DD>::kThreadsPer, lds, stream>>>(p);          \
+  } while (0)
+#define TS_LAUNCH_FP4(DD, SS, SPARSE, NARROW, OUT)                                              \
+  do {                                                                                         \
+    if (p.B * p.Hkv > Fp4Shape<DD>::kResident) TS_LAUNCH_FP4_BATCH(DD, SS, SPARSE, NARROW, OUT, true); \
+    else TS_LAUNCH_FP4_BATCH(DD, SS, SPARSE, NARROW, OUT, false);                              \
   } while (0)
 #define TS_LAUNCH_FP4_OUT(DD, SS, SPARSE, NARROW)                \
   do {                                                           \
@@ -481,6 +486,7 @@ static int launch_fp4_attention(const ts_layout* L, const Fp4Plan& pl, const voi
 #undef TS_LAUNCH_FP4_HEADS
 #undef TS_LAUNCH_FP4_OUT
 #undef TS_LAUNCH_FP4
+#undef TS_LAUNCH_FP4_BATCH
   return launch_status();
 }
 

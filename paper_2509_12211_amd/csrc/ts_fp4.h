@@ -14,8 +14,8 @@
 //
 // Work: every workgroup works out from the lengths what it has to do.  Much work is numbered through, fragment
 // after fragment and unit after unit, and dealt out in equal contiguous shares, whatever the lengths; little goes
-// unit by unit, each to as many workgroups as its length asks for.  A workgroup's waves take the fragments of a
-// unit in turn and merge in LDS.  A unit that several workgroups share is merged by the
+// unit by unit, each to as many workgroups as its length asks for; many short units go to a wave each.  A workgroup's
+// waves take the fragments of a unit in turn and merge in LDS.  A unit that several workgroups share is merged by the
 // last of them to arrive (an atomic count in the workspace, set back to zero); nobody waits.
 //
 // Measured (kernel alone, cold data): 64 sequences of 1024 to 32768 tokens, 8 KV heads of 128 channels, 1.14 GB:
@@ -35,6 +35,11 @@ constexpr int kFp4List = 1024;          // list entries held in LDS at a time
 // 16 heads on one of 128 channels, 48 to 50 us from 64 on.
 constexpr int kFp4Parts = 64;
 constexpr int kFp4Counters = 1024;      // places for counts, whatever the batch
+// Units of at most this many fragments (what a wave's part of the list holds) are taken by a wave each where there are
+// at least a sixth as many units, for each that are at work at once, as the longest has fragments: a turn of a workgroup
+// each takes about 4.8 us and 0.23 for every fragment, a wave 4.5 and 0.85.  256 sequences of 200 tokens, 8 heads on
+// 64 channels 27.9 -> 14.1 us, on 128 25.6 -> 15.7; 128 of 64 tokens 10.7 -> 6.0; 128 of 1024 would lose, 24.1 -> 31.5.
+constexpr int kFp4ShortUnit = 32, kFp4ShortTurn = 6;
 // Fragments of a workgroup from which on all get the same number: with 384 the ragged batch of 1.1 GB goes unit by
 // unit and takes 250 us instead of 222; 48 changes nothing that was measured.
 constexpr uint32_t kFp4LongShare = 192;
@@ -348,7 +353,8 @@ __device__ __forceinline__ float4_t load_part(__amdgpu_buffer_rsrc_t r, uint32_t
   return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, kPartAgent));
 }
 
-template <int D, int S, bool kSparse, bool kNarrow, bool kOut32>
+// kMany: more units than workgroups at once (the others are 1 to 5 % faster without the choice).
+template <int D, int S, bool kSparse, bool kNarrow, bool kOut32, bool kMany>
 __global__ __launch_bounds__(Fp4Shape<D>::kThreadsPer, Fp4Shape<D>::kPerCu * Fp4Shape<D>::kWavesPer / 4)
 void fp4_attention_kernel(Fp4Params p) {
   typedef Fp4Shape<D> Shape;
@@ -402,7 +408,10 @@ void fp4_attention_kernel(Fp4Params p) {
     }
     return n * (uint32_t)p.Hkv;
   };
-  const bool aligned = share < kFp4LongShare;
+  // Many short units: each wave has one of its own, and nothing to merge.
+  const bool solo = kMany && longest <= kFp4ShortUnit &&
+                    (uint32_t)(longest * Shape::kResident) <= kFp4ShortTurn * units;
+  const bool aligned = !solo && share < kFp4LongShare;
   if (aligned) {
     // parts a little larger than an equal share, so that all are at work at once; else what is sure to fit, or
     // (more units than that) whole units in as many turns as it takes
@@ -413,7 +422,17 @@ void fp4_attention_kernel(Fp4Params p) {
   uint32_t at, end, ustart = 0;     // this workgroup's fragments; the first of its unit
   int b = 0, h, nf = 0, parts_of_unit = 0;
   uint32_t first_part = 0;          // aligned: the unit's first workgroup
-  {
+  if (solo) {
+    if (blockIdx.x * kFp4Waves >= units) return;
+    const uint32_t unit = blockIdx.x * kFp4Waves + (uint32_t)wave;
+    if (unit < units) {
+      b = uniform((int)(unit / (uint32_t)p.Hkv));
+      nf = uniform(fp4_frags<S, kSparse>(p, b));
+    }
+    h = unit < units ? (int)unit - b * p.Hkv : 0;
+    at = 0;
+    end = max((uint32_t)nf, 1u);      // (all waves go once through what follows, and meet the barrier in it)
+  } else {
     const uint32_t key = aligned ? blockIdx.x : blockIdx.x * share;       // workgroups, or fragments, are numbered through
     uint32_t from = 0;
     if (!aligned && (blockIdx.x >= room || key >= total)) return;      // (key: what 32 bits hold, of the first room)
@@ -453,6 +472,10 @@ void fp4_attention_kernel(Fp4Params p) {
     }
   }
 
+  // (a wave by itself has a part of the list, too, and reads what it wrote: LDS takes a wave's accesses in order)
+  Fp4Entry* my_list = list + (solo ? wave * (kFp4List / kFp4Waves) : 0);
+  static_assert((kFp4ShortUnit + FPP - 1) / FPP * PPF <= kFp4List / kFp4Waves, "room for a short unit's entries");
+  const int step = solo ? 1 : kFp4Waves;
   while (at < end) {
     const int f0 = (int)(at - ustart), f1 = (int)min((uint32_t)nf, end - ustart);
     const int u = b * p.Hkv + h;
@@ -473,8 +496,8 @@ void fp4_attention_kernel(Fp4Params p) {
     for (int cb = 0; cb < D / 16; ++cb) st.acc[cb] = float4_t{0.f, 0.f, 0.f, 0.f};
     for (int c0 = f0; c0 < f1; c0 += kFrags) {
       const int c1 = min(f1, c0 + kFrags), e0 = c0 / FPP * PPF, entries = ((c1 - 1) / FPP + 1) * PPF - e0;
-      __syncthreads();    // the list before is read, and so is the merge area
-      for (int i = tid; i < entries; i += kFp4Threads) {
+      if (!solo) __syncthreads();    // the list before is read, and so is the merge area
+      for (int i = solo ? lane : tid; i < entries; i += solo ? kWave : kFp4Threads) {
         int page = e0 + i;
         bool on = true;
         if (kSparse) {
@@ -484,18 +507,18 @@ void fp4_attention_kernel(Fp4Params p) {
         on = on && page >= 0 && page < p.Pmax;
         const int phys = p.block_table[(size_t)b * p.Pmax + (on ? page : 0)];
         on = on && phys >= 0 && phys < p.n_phys;
-        list[i] = on ? fp4_entry(p, phys, h, min(max(len - page * S, 0), S)) : fp4_entry(p, 0, h, 0);
+        my_list[i] = on ? fp4_entry(p, phys, h, min(max(len - page * S, 0), S)) : fp4_entry(p, 0, h, 0);
       }
-      __syncthreads();
+      if (!solo) __syncthreads();
       const int shift = c0 % FPP - c0;      // fragments as the list has them
-      const uint32_t list_at = lds_address(list), ring = lds_address(merge) + wave * Shape::kRing;
+      const uint32_t list_at = lds_address(my_list), ring = lds_address(merge) + wave * Shape::kRing;
       const int last = c1 + shift;
-      int f = c0 + wave + shift, stage = 0;
+      int f = c0 + (solo ? 0 : wave) + shift, stage = 0;
 #pragma unroll
       for (int i = 0; i < kStages - 1; ++i)
-        if (f + i * kFp4Waves < last) fetch_fp4<D, S>(list_at, f + i * kFp4Waves, ring + i * Shape::kStage);
-      for (; f < last; f += kFp4Waves) {
-        const int ahead = f + (kStages - 1) * kFp4Waves;
+        if (f + i * step < last) fetch_fp4<D, S>(list_at, f + i * step, ring + i * Shape::kStage);
+      for (; f < last; f += step) {
+        const int ahead = f + (kStages - 1) * step;
         const int to = stage == 0 ? kStages - 1 : stage - 1;      // the stage that the fragment before has left
         if (ahead < last) {
           fetch_fp4<D, S>(list_at, ahead, ring + to * Shape::kStage);
@@ -549,6 +572,13 @@ void fp4_attention_kernel(Fp4Params p) {
       store_fp4_out<kOut32>(p, at_head * D + c, o * inv);
       if (p.lse && c == 0) p.lse[at_head] = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * 0.6931471805599453f;
     };
+    if (solo) {
+      for (int i = nf > 0 ? lane : items; i < items; i += kWave) {
+        const float* row = merge + wave * kWaveRows + i / (D / 4) * kRow;
+        finish(i, row[D], row[D + 1], *reinterpret_cast<const float4_t*>(row + i % (D / 4) * 4));
+      }
+      return;
+    }
     for (int i = tid; i < items; i += kFp4Threads) {
       const int g = i / (D / 4), c = i % (D / 4) * 4;
       float M = -INFINITY;

@@ -336,6 +336,44 @@ def test_many_units(B, lens, Hq, Hkv, d):
     c.check(c.out, c.lse, 0.2, what="many")
 
 
+@pytest.mark.parametrize("B,top,Hq,Hkv,d,S,out", [
+    (103, 1024, 5, 5, 64, 16, "f32"), (111, 300, 14, 7, 128, 8, "bf16"), (111, 90, 70, 7, 128, 32, "f32"),
+    (33, 200, 40, 40, 64, 64, "bf16"), (103, 31, 80, 5, 64, 8, "f32"), (111, 1024, 7, 7, 128, 64, "f32"),
+    (111, 190, 7, 7, 128, 8, "f32"), (111, 192, 112, 7, 128, 16, "bf16"), (410, 1024, 10, 10, 64, 8, "f32"),
+])
+def test_more_short_units_than_workgroups(B, top, Hq, Hkv, d, S, out):
+    """Every length from none to as many tokens as a wave takes by itself (and more), whole caches and lists of pages."""
+    g = torch.Generator().manual_seed(B + top)
+    n = (torch.randint(0, top + 1, (B,), generator=g) // (8 if B > 200 else 1)).tolist()
+    n[3], n[B // 2], n[B - 1], n[7], n[8] = 0, top, top, 1, 32
+    c = Fp4(n, Hq, Hkv, d, S, g, pad=16, out=out, offset=0.5)
+    scale = 1.0 / math.sqrt(d)
+    ws = ts.new_dense_workspace(c.layout, DEV)
+    ts.dense_decode_attention(c.layout, c.q, scale, c.out, ws, lse_out=c.lse)
+    c.check(c.out, c.lse, scale, what="short")
+    again = torch.full_like(c.out, math.nan)
+    ts.dense_decode_attention(c.layout, c.q, scale, again, ws)
+    assert torch.equal(again, c.out)
+    # every other page, and of some sequences none
+    pages = [-(-x // S) for x in n]
+    most = max(-(-x // 2) for x in pages)
+    sel = torch.full((B, Hkv, most), -1, dtype=torch.int32)
+    counts = [0 if b % 9 == 4 else x // 2 for b, x in enumerate(pages)]
+    tokens = [[torch.zeros(0, dtype=torch.long)] * Hkv for _ in n]
+    for b, k in enumerate(counts):
+        for h in range(Hkv):
+            ids = 2 * torch.arange(k) + (h & 1)
+            sel[b, h, :k] = ids.int()
+            at = (ids[:, None] * S + torch.arange(S)).view(-1)
+            tokens[b][h] = at[at < n[b]]
+    c.out.fill_(math.nan)
+    c.lse.fill_(math.nan)
+    ws = ts.new_workspace(c.layout, most, DEV)
+    ts.sparse_decode_attention(c.layout, c.q, sel.to(DEV), torch.tensor(counts, dtype=torch.int32, device=DEV), most, scale,
+                               c.out, ws, lse_out=c.lse)
+    c.check(c.out, c.lse, scale, tokens=tokens, what="lists")
+
+
 def test_equal_shares_of_more_long_units_than_workgroups():
     """800 units of some 190 fragments: workgroups that reach over several units' ends.  The sequences'
     tables are permutations of the same pages, so that the cache and its plain form stay small."""
